@@ -57,7 +57,7 @@ typedef enum {
     DIROTQ_ERR_DEVICE_TIMEOUT = 6  /* a bounded device-side wait expired */
 } dirotq_status_t;
 
-enum { DIROTQ_DTYPE_F32 = 0, DIROTQ_DTYPE_BF16 = 1, DIROTQ_DTYPE_F64 = 2 };
+enum { DIROTQ_DTYPE_F32 = 0, DIROTQ_DTYPE_BF16 = 1, DIROTQ_DTYPE_F64 = 2, DIROTQ_DTYPE_F16 = 3 };
 enum { DIROTQ_LAYOUT_KN = 0 /* W[k*N + n] */, DIROTQ_LAYOUT_NK = 1 /* W[n*K + k] */ };
 
 /* Human-readable name of a status code (static string, never NULL). */
@@ -441,6 +441,112 @@ DIROTQ_API dirotq_status_t dirotq_act_scale_log2_from_rotated(const float* xrot_
 DIROTQ_API dirotq_status_t dirotq_act_scale_log2_ph(const void* x, int M, const void* Uh, int uh_dtype, int K, int r,
                                                     void* scratch, size_t scratch_bytes, int* act_scale_log2,
                                                     dirotq_stream_t stream);
+
+/* ---- MXFP4: 4-bit floats with a power-of-two scale per 32 (OCP Microscaling Formats; no counterpart in the paper, whose 4-bit
+ * float setting is NVFP4).  Quantized operands of their own, without a rotation: a layer in this format needs no calibration, and
+ * checkpoints come in it ----
+ *
+ * An operand is a matrix [rows, K] quantized along K.  Blocks of 32 consecutive elements of a row share one scale 2^e, kept as the
+ * byte e + 127 (E8M0); elements are E2M1 codes (bit 3 sign, bits 2..0 index into {0, .5, 1, 1.5, 2, 3, 4, 6}).  With a = max|x| of
+ * the block (the last block of a row may be ragged)
+ *     DIROTQ_MX_SCALE_FLOOR:  e = floor(log2 a) - 2, the rule of the OCP specification (elements above 6 * 2^e saturate);
+ *     DIROTQ_MX_SCALE_CEIL:   the smallest e with a <= 6 * 2^e (nothing saturates);
+ * e is at least -127; a block of zeros has e = -127.  code = E2M1 of x 2^-e to nearest, ties to the even code, sign kept.  A block
+ * that holds an infinity or a NaN becomes scale 255 (NaN) with codes 0, and stands for NaN everywhere it is used.
+ *
+ * rows >= 1, 1 <= K <= 1048576, rows <= 16777216.  Strides (ldx, ldy) are in elements and at least the width of a row; rows of any
+ * alignment are taken (16-byte aligned ones are read and written in wide pieces).  The calls follow the conventions at the top:
+ * the current device must be the one the operand was created on. */
+typedef struct dirotq_mxfp4 dirotq_mxfp4_t; /* opaque host-side handle of a quantized operand */
+enum { DIROTQ_MX_SCALE_FLOOR = 0, DIROTQ_MX_SCALE_CEIL = 1 };
+
+/* Bytes of the device buffer of an operand: codes (rows * ceil(K/32) * 16) and scales in the tensor core's order (rows rounded up to
+ * 256, K to 256; one byte per 32). */
+DIROTQ_API dirotq_status_t dirotq_mxfp4_bytes(int rows, int K, size_t* bytes);
+/* Host handle of an operand in `buffer` (device, 1024-byte aligned, must outlive the handle).  Launches nothing; the contents are
+ * undefined until the operand is quantized or imported. */
+DIROTQ_API dirotq_status_t dirotq_mxfp4_create(int rows, int K, void* buffer, size_t buffer_bytes, dirotq_mxfp4_t** out);
+/* Frees the host handle (not the buffer). */
+DIROTQ_API dirotq_status_t dirotq_mxfp4_destroy(dirotq_mxfp4_t* t);
+DIROTQ_API dirotq_status_t dirotq_mxfp4_info(const dirotq_mxfp4_t* t, int* rows, int* K);
+
+/* Quantizes x (dtype F32, BF16 or F16) into the operand.  x_layout as for weights: DIROTQ_LAYOUT_NK, x[row*ldx + k] (activations, and
+ * weights stored [N,K]); DIROTQ_LAYOUT_KN, x[k*ldx + row] (weights stored [K,N]). */
+DIROTQ_API dirotq_status_t dirotq_mxfp4_quantize(const void* x, int x_dtype, int x_layout, long long ldx, int scale_rule,
+                                                 const dirotq_mxfp4_t* out, dirotq_stream_t stream);
+/* y[row*ldy + k] = the value the operand's element stands for, rounded once to y_dtype (F32, BF16 or F16). */
+DIROTQ_API dirotq_status_t dirotq_mxfp4_dequantize(const dirotq_mxfp4_t* t, void* y, int y_dtype, long long ldy,
+                                                   dirotq_stream_t stream);
+/* The plain form that checkpoints hold: codes u8 [rows, ceil(K/2)], the even element in the low half of a byte; scales u8
+ * [rows, ceil(K/32)].  Both DEVICE, row-major, any alignment.  (The spare half-byte of an odd K is ignored and exported as 0.) */
+DIROTQ_API dirotq_status_t dirotq_mxfp4_import(const uint8_t* codes, const uint8_t* scales, const dirotq_mxfp4_t* out,
+                                               dirotq_stream_t stream);
+DIROTQ_API dirotq_status_t dirotq_mxfp4_export(const dirotq_mxfp4_t* t, uint8_t* codes, uint8_t* scales, dirotq_stream_t stream);
+
+/* y[m*ldy + n] = a[m,:] . b[n,:] + bias[n] for operands a [M,K] and b [N,K]: the block scales are applied inside the tensor core
+ * (tcgen05.mma kind::mxf4), sums are held in fp32 and rounded once to y_dtype (BF16 or F16).  bias: DEVICE [N] in y's dtype, or NULL.
+ * workspace: at least 256 bytes, 16-byte aligned, zero-filled once before its first use (dirotq_workspace_status reads it).
+ * An output row's bits do not depend on how many rows the call has. */
+DIROTQ_API dirotq_status_t dirotq_mxfp4_gemm(const dirotq_mxfp4_t* a, const dirotq_mxfp4_t* b, const void* bias, void* y, int y_dtype,
+                                             long long ldy, void* workspace, size_t workspace_bytes, dirotq_stream_t stream);
+
+/* A linear layer on a quantized weight w [N,K]: x (F32, BF16 or F16, x[m*ldx + k]) is quantized into the workspace, then
+ * dirotq_mxfp4_gemm.  workspace: dirotq_mxfp4_workspace_bytes(M, K) bytes (enough for any smaller M too), 1024-byte aligned,
+ * zero-filled once before its first use; calls that may overlap need distinct ones. */
+DIROTQ_API dirotq_status_t dirotq_mxfp4_workspace_bytes(int M, int K, size_t* bytes);
+DIROTQ_API dirotq_status_t dirotq_mxfp4_linear(const void* x, int x_dtype, long long ldx, int M, int scale_rule, const dirotq_mxfp4_t* w,
+                                               const void* bias, void* y, int y_dtype, long long ldy, void* workspace,
+                                               size_t workspace_bytes, dirotq_stream_t stream);
+
+/* ---- queries and keys behind a fused q/k/v projection (no counterpart in the paper: what the transformers whose linears this
+ * library quantizes do with that projection's output before attention) ----
+ *
+ * A row of x is [heads_q | heads_kv | heads_kv] heads of head_dim elements: q, k, v of one token.  For every head h of q and k
+ *     n = h / sqrt(mean(h^2) + eps) * w           (w: q_weight for q, k_weight for k; norm == 0 skips this line)
+ * and the first rot_dim elements of n are rotated in pairs (a, b) by the angle of the token's position p, c = cos_table[p][i],
+ * s = sin_table[p][i], pair i:   (a, b) -> (a c - b s, a s + b c)
+ *     DIROTQ_ROPE_PAIRS:  a = n[2i], b = n[2i+1];      DIROTQ_ROPE_HALVES:  a = n[i], b = n[i + rot_dim/2].
+ * v is not changed.  Everything is computed in fp32 (the sum of squares too: |x| up to 1e18) and rounded once. */
+enum { DIROTQ_ROPE_NONE = 0, DIROTQ_ROPE_PAIRS = 1, DIROTQ_ROPE_HALVES = 2 };
+typedef struct {
+    int heads_q, heads_kv, head_dim; /* head_dim a multiple of 8, at most 256 */
+    int norm;                        /* 1: RMS norm of every head, 0: none */
+    float eps;                       /* >= 0 */
+    int weight_dtype;                /* F32, BF16 or F16: the two weights below */
+    const void* q_weight;            /* DEVICE [head_dim], or NULL (ones) */
+    const void* k_weight;
+    int rope;                        /* DIROTQ_ROPE_* */
+    int rot_dim;                     /* even, 2..head_dim (0 with DIROTQ_ROPE_NONE) */
+    const float* cos_table;          /* DEVICE fp32 [num_positions][ld_table], the first rot_dim/2 of a row are used */
+    const float* sin_table;
+    long long ld_table;
+    int num_positions;
+    const int32_t* positions;        /* DEVICE [M], or NULL: token m has position m (then num_positions >= M) */
+} dirotq_qk_t;
+
+/* x, q_out, k_out, v_out: one dtype (F32, BF16 or F16), 16-byte aligned, row strides ldx, ldq, ldk, ldv multiples of 8 elements.
+ * q of token m goes to row m of q_out [M][ldq], k and v to row m of k_out and v_out, or, with slots (DEVICE int32 [M]), to row
+ * slots[m] of k_out / v_out [num_slots][ldk / ldv], e.g. of a cache.  v_out == NULL: v is not copied.
+ * In place: q_out == x, k_out == x + heads_q*head_dim elements, the same strides and no slots (and v_out NULL, or v's own place).
+ * Any other overlap of an output with x is refused, as far as addresses tell.
+ * Padding: a token whose position is outside [0, num_positions) or whose slot is outside [0, num_slots) is left out altogether;
+ * nothing of it is written.  Slots of different tokens must differ (rows written twice hold a mixture of the two). */
+DIROTQ_API dirotq_status_t dirotq_qk_norm_rope(const void* x, int dtype, int M, long long ldx, const dirotq_qk_t* qk, void* q_out,
+                                               long long ldq, void* k_out, long long ldk, void* v_out, long long ldv,
+                                               const int32_t* slots, int num_slots, dirotq_stream_t stream);
+
+/* dirotq_linear on a layer (of any format) whose N columns are q, k and v of a token, then dirotq_qk_norm_rope in place on y:
+ * N == (heads_q + 2 heads_kv) * head_dim. */
+DIROTQ_API dirotq_status_t dirotq_linear_qkv(const void* x, int M, const dirotq_layer_t* layer, const dirotq_qk_t* qk, void* y,
+                                             void* workspace, size_t workspace_bytes, dirotq_stream_t stream);
+
+/* dirotq_mxfp4_linear on a fused q/k/v weight with norm and rotation in the product's epilogue: y = [q | k | v], rounded once.
+ * head_dim 64 or 128, rot_dim 0 or head_dim; other heads: DIROTQ_ERR_UNSUPPORTED_SHAPE (dirotq_mxfp4_linear and dirotq_qk_norm_rope
+ * serve those).  q and k of a token whose position is outside [0, num_positions) stay what the projection made them, as behind
+ * dirotq_linear_qkv. */
+DIROTQ_API dirotq_status_t dirotq_mxfp4_qkv(const void* x, int x_dtype, long long ldx, int M, int scale_rule, const dirotq_mxfp4_t* w,
+                                            const void* bias, const dirotq_qk_t* qk, void* y, int y_dtype, long long ldy,
+                                            void* workspace, size_t workspace_bytes, dirotq_stream_t stream);
 
 /* ---- failure-path check (no counterpart in the paper) ---------------------------------------- */
 

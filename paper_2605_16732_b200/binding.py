@@ -19,8 +19,9 @@ _LIB_PATH = os.environ.get("DIROTQ_LIBRARY") or os.path.join(os.path.dirname(os.
 DIROTQ_OK = 0
 STATUS_NAMES = {0: "ok", 1: "invalid argument", 2: "unsupported shape", 3: "buffer too small",
                 4: "device is not sm_100", 5: "CUDA error", 6: "device-side wait timed out"}
-DTYPE_F32, DTYPE_BF16, DTYPE_F64 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_F64, DTYPE_F16 = 0, 1, 2, 3
 LAYOUT_KN, LAYOUT_NK = 0, 1
+MX_SCALE_FLOOR, MX_SCALE_CEIL = 0, 1
 
 EXPORTED = [
     "dirotq_status_string", "dirotq_version", "dirotq_last_error", "dirotq_layer_bytes",
@@ -32,6 +33,9 @@ EXPORTED = [
     "dirotq_layer_bytes_w4a8", "dirotq_prepare_layer_w4a8", "dirotq_workspace_export_w4a8",
     "dirotq_prepare_layer_codes", "dirotq_prepare_scratch_bytes_gptq", "dirotq_prepare_layer_gptq", "dirotq_layer_bytes_ph", "dirotq_prepare_scratch_bytes_ph", "dirotq_prepare_layer_ph",
     "dirotq_layer_export_uh", "dirotq_layer_export_v", "dirotq_layer_bytes_nvfp4_ph", "dirotq_prepare_layer_nvfp4_ph", "dirotq_layer_bytes_sibling", "dirotq_prepare_layer_sibling", "dirotq_set_gemm_tile", "dirotq_set_dependent_launch", "dirotq_set_rotation_tile", "dirotq_set_first_step_split", "dirotq_layer_bytes_asym", "dirotq_prepare_layer_asym", "dirotq_workspace_export_asym", "dirotq_layer_export_zero_term",
+    "dirotq_mxfp4_bytes", "dirotq_mxfp4_create", "dirotq_mxfp4_destroy", "dirotq_mxfp4_info", "dirotq_mxfp4_quantize", "dirotq_mxfp4_dequantize",
+    "dirotq_mxfp4_import", "dirotq_mxfp4_export", "dirotq_mxfp4_gemm", "dirotq_mxfp4_workspace_bytes", "dirotq_mxfp4_linear", "dirotq_mxfp4_qkv",
+    "dirotq_qk_norm_rope", "dirotq_linear_qkv",
 ]
 
 
@@ -115,6 +119,21 @@ def lib() -> ctypes.CDLL:
                                                  ctypes.POINTER(vp)]
         L.dirotq_workspace_export_asym.argtypes = [vp, i, vp, vp, vp, vp, vp, vp]
         L.dirotq_layer_export_zero_term.argtypes = [vp, vp, vp]
+        ll = ctypes.c_longlong
+        L.dirotq_mxfp4_bytes.argtypes = [i, i, psz]
+        L.dirotq_mxfp4_create.argtypes = [i, i, vp, sz, ctypes.POINTER(vp)]
+        L.dirotq_mxfp4_destroy.argtypes = [vp]
+        L.dirotq_mxfp4_info.argtypes = [vp, pi, pi]
+        L.dirotq_mxfp4_quantize.argtypes = [vp, i, i, ll, i, vp, vp]
+        L.dirotq_mxfp4_dequantize.argtypes = [vp, vp, i, ll, vp]
+        L.dirotq_mxfp4_import.argtypes = [vp, vp, vp, vp]
+        L.dirotq_mxfp4_export.argtypes = [vp, vp, vp, vp]
+        L.dirotq_mxfp4_gemm.argtypes = [vp, vp, vp, vp, i, ll, vp, sz, vp]
+        L.dirotq_mxfp4_workspace_bytes.argtypes = [i, i, psz]
+        L.dirotq_mxfp4_linear.argtypes = [vp, i, ll, i, i, vp, vp, vp, i, ll, vp, sz, vp]
+        L.dirotq_mxfp4_qkv.argtypes = [vp, i, ll, i, i, vp, vp, vp, vp, i, ll, vp, sz, vp]
+        L.dirotq_qk_norm_rope.argtypes = [vp, i, i, ll, vp, vp, ll, vp, ll, vp, ll, vp, i, vp]
+        L.dirotq_linear_qkv.argtypes = [vp, i, vp, vp, vp, vp, sz, vp]
         for name in EXPORTED:
             if name not in ("dirotq_status_string", "dirotq_version", "dirotq_last_error"):
                 getattr(L, name).restype = i
@@ -655,3 +674,184 @@ def dirotq_workspace_export_w4a8(layer: Layer, M: int, workspace: torch.Tensor, 
     _check(lib().dirotq_workspace_export_w4a8(layer.handle, M, workspace.data_ptr(), xh.data_ptr(), codes.data_ptr(),
                                               scales.data_ptr(), _stream(stream)), "dirotq_workspace_export_w4a8")
     return xh, codes, scales
+
+
+# ------------------------------------------------------------------ MXFP4
+
+_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+
+
+def _row_stride(t: torch.Tensor, width: int) -> int:
+    """Elements between the rows of a 2-D tensor whose rows are contiguous.  A single row's stride says nothing: one that would keep the
+    library from wide accesses, or is shorter than the row, is replaced."""
+    assert t.is_cuda and t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1), "rows must be contiguous"
+    if t.shape[0] > 1 or (t.stride(0) >= width and t.stride(0) % 8 == 0):
+        return t.stride(0)
+    return (max(width, t.shape[1]) + 7) // 8 * 8
+
+
+class Mxfp4:
+    """Owner of one quantized operand [rows, K]: the device buffer (a torch uint8 tensor) and the host handle."""
+
+    def __init__(self, handle: int, buffer: torch.Tensor, rows: int, K: int):
+        self.handle, self.buffer = handle, buffer
+        self.rows, self.K = rows, K
+
+    def close(self):
+        if self.handle:
+            lib().dirotq_mxfp4_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def dirotq_mxfp4_bytes(rows: int, K: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().dirotq_mxfp4_bytes(rows, K, ctypes.byref(out)), "dirotq_mxfp4_bytes")
+    return out.value
+
+
+def dirotq_mxfp4_alloc(rows: int, K: int, device="cuda") -> Mxfp4:
+    """An operand with a buffer of its own; its contents are undefined until it is quantized or imported."""
+    buffer = _alloc_bytes(dirotq_mxfp4_bytes(rows, K), device)
+    handle = ctypes.c_void_p(0)
+    _check(lib().dirotq_mxfp4_create(rows, K, buffer.data_ptr(), buffer.numel(), ctypes.byref(handle)), "dirotq_mxfp4_create")
+    return Mxfp4(handle.value, buffer, rows, K)
+
+
+def dirotq_mxfp4_quantize(x: torch.Tensor, out: Mxfp4 | None = None, scale_rule: int = MX_SCALE_FLOOR, layout: int = LAYOUT_NK,
+                          stream=None) -> Mxfp4:
+    """x: cuda float32/bfloat16/float16 [rows, K] (LAYOUT_NK) or [K, rows] (LAYOUT_KN), rows of any stride."""
+    rows, K = (x.shape[0], x.shape[1]) if layout == LAYOUT_NK else (x.shape[1], x.shape[0])
+    if out is None:
+        out = dirotq_mxfp4_alloc(rows, K, x.device)
+    assert (out.rows, out.K) == (rows, K), "the operand has another shape"
+    _check(lib().dirotq_mxfp4_quantize(x.data_ptr(), _DTYPES[x.dtype], layout, _row_stride(x, x.shape[1]), scale_rule, out.handle,
+                                       _stream(stream)), "dirotq_mxfp4_quantize")
+    return out
+
+
+def dirotq_mxfp4_dequantize(t: Mxfp4, y: torch.Tensor, stream=None) -> None:
+    assert tuple(y.shape) == (t.rows, t.K)
+    _check(lib().dirotq_mxfp4_dequantize(t.handle, y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, t.K), _stream(stream)),
+           "dirotq_mxfp4_dequantize")
+
+
+def dirotq_mxfp4_import(codes: torch.Tensor, scales: torch.Tensor, K: int, out: Mxfp4 | None = None, stream=None) -> Mxfp4:
+    """codes: cuda uint8 [rows, ceil(K/2)], the even element in the low half of a byte; scales: cuda uint8 [rows, ceil(K/32)]."""
+    rows = codes.shape[0]
+    assert codes.is_cuda and codes.is_contiguous() and codes.dtype == torch.uint8 and tuple(codes.shape) == (rows, -(-K // 2))
+    assert scales.is_cuda and scales.is_contiguous() and scales.dtype == torch.uint8 and tuple(scales.shape) == (rows, -(-K // 32))
+    if out is None:
+        out = dirotq_mxfp4_alloc(rows, K, codes.device)
+    assert (out.rows, out.K) == (rows, K), "the operand has another shape"
+    _check(lib().dirotq_mxfp4_import(codes.data_ptr(), scales.data_ptr(), out.handle, _stream(stream)), "dirotq_mxfp4_import")
+    return out
+
+
+def dirotq_mxfp4_export(t: Mxfp4, stream=None):
+    codes = torch.empty((t.rows, -(-t.K // 2)), dtype=torch.uint8, device=t.buffer.device)
+    scales = torch.empty((t.rows, -(-t.K // 32)), dtype=torch.uint8, device=t.buffer.device)
+    _check(lib().dirotq_mxfp4_export(t.handle, codes.data_ptr(), scales.data_ptr(), _stream(stream)), "dirotq_mxfp4_export")
+    return codes, scales
+
+
+def alloc_mxfp4_workspace(M: int, K: int, device="cuda") -> torch.Tensor:
+    """Workspace of the MXFP4 products of up to M rows of K elements."""
+    out = ctypes.c_size_t(0)
+    _check(lib().dirotq_mxfp4_workspace_bytes(M, K, ctypes.byref(out)), "dirotq_mxfp4_workspace_bytes")
+    return _alloc_bytes(out.value, device, zero=True)
+
+
+def _check_bias(bias, y):
+    assert bias is None or (bias.is_cuda and bias.is_contiguous() and bias.dtype == y.dtype and bias.numel() == y.shape[1])
+
+
+def dirotq_mxfp4_gemm(a: Mxfp4, b: Mxfp4, y: torch.Tensor, workspace: torch.Tensor, bias: torch.Tensor | None = None, stream=None) -> None:
+    """y [a.rows, b.rows] (bf16 or f16, rows of any stride) = a b^T + bias."""
+    assert tuple(y.shape) == (a.rows, b.rows)
+    _check_bias(bias, y)
+    _check(lib().dirotq_mxfp4_gemm(a.handle, b.handle, _ptr(bias), y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, b.rows), workspace.data_ptr(),
+                                   workspace.numel(), _stream(stream)), "dirotq_mxfp4_gemm")
+
+
+def dirotq_mxfp4_linear(x: torch.Tensor, w: Mxfp4, y: torch.Tensor, workspace: torch.Tensor, bias: torch.Tensor | None = None,
+                        scale_rule: int = MX_SCALE_FLOOR, stream=None) -> None:
+    """y [M, w.rows] (bf16 or f16) = x w^T + bias with x [M, K] quantized on the way in."""
+    assert x.shape[1] == w.K and tuple(y.shape) == (x.shape[0], w.rows)
+    _check_bias(bias, y)
+    _check(lib().dirotq_mxfp4_linear(x.data_ptr(), _DTYPES[x.dtype], _row_stride(x, w.K), x.shape[0], scale_rule, w.handle, _ptr(bias), y.data_ptr(),
+                                     _DTYPES[y.dtype], _row_stride(y, w.rows), workspace.data_ptr(), workspace.numel(), _stream(stream)),
+           "dirotq_mxfp4_linear")
+
+
+# ------------------------------------------------------------------ queries and keys
+
+class _QkStruct(ctypes.Structure):
+    _fields_ = [("heads_q", ctypes.c_int), ("heads_kv", ctypes.c_int), ("head_dim", ctypes.c_int), ("norm", ctypes.c_int), ("eps", ctypes.c_float),
+                ("weight_dtype", ctypes.c_int), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("rope", ctypes.c_int),
+                ("rot_dim", ctypes.c_int), ("cos_table", ctypes.c_void_p), ("sin_table", ctypes.c_void_p), ("ld_table", ctypes.c_longlong),
+                ("num_positions", ctypes.c_int), ("positions", ctypes.c_void_p)]
+
+
+class QkNorm:
+    """What is done to the heads of q and k (dirotq_qk_t), and the tensors it refers to.
+
+    rope: "pairs" (elements 2i, 2i+1), "halves" (i, i + rot_dim/2) or None; cos, sin: cuda float32 [positions, rot_dim/2]; positions: cuda
+    int32 [M], or None (row m has position m); q_weight, k_weight: cuda [head_dim], or None (ones)."""
+
+    def __init__(self, heads_q: int, heads_kv: int, head_dim: int, q_weight=None, k_weight=None, eps: float = 1e-6, norm: bool = True,
+                 rope: str | None = None, rot_dim: int | None = None, cos=None, sin=None, positions=None):
+        self.heads_q, self.heads_kv, self.head_dim = heads_q, heads_kv, head_dim
+        style = {None: 0, "pairs": 1, "halves": 2}[rope]
+        rot = 0 if style == 0 else head_dim if rot_dim is None else rot_dim
+        if rot == 0:
+            style, cos, sin, positions = 0, None, None, None
+        weights = [w for w in (q_weight, k_weight) if w is not None]
+        for w in weights:
+            assert w.is_cuda and w.is_contiguous() and w.numel() == head_dim and w.dtype == weights[0].dtype
+        if style:
+            assert cos.is_cuda and sin.is_cuda and cos.dtype == sin.dtype == torch.float32 and cos.shape == sin.shape and cos.shape[1] >= rot // 2
+            assert cos.stride() == sin.stride() and (cos.stride(1) == 1 or cos.shape[1] == 1)
+            assert positions is None or (positions.is_cuda and positions.is_contiguous() and positions.dtype == torch.int32 and positions.dim() == 1)
+        self.positions = positions
+        self._keep = (q_weight, k_weight, cos, sin, positions)
+        self.struct = _QkStruct(heads_q, heads_kv, head_dim, int(norm), float(eps), _DTYPES[weights[0].dtype] if weights else DTYPE_F32, _ptr(q_weight),
+                                _ptr(k_weight), style, rot, _ptr(cos), _ptr(sin), _row_stride(cos, rot // 2) if style else 0, cos.shape[0] if style else 0,
+                                _ptr(positions))
+
+    def _ref(self, M: int):
+        assert self.positions is None or self.positions.numel() == M, "one position per token"
+        return ctypes.byref(self.struct)
+
+
+def dirotq_qk_norm_rope(x: torch.Tensor, qk: QkNorm, q_out: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor | None = None,
+                        slots: torch.Tensor | None = None, stream=None) -> None:
+    """x [M, (heads_q + 2 heads_kv) head_dim]; q_out [M, heads_q head_dim]; k_out, v_out [M or slots, heads_kv head_dim]; slots: cuda int32 [M]."""
+    M, wq, wk = x.shape[0], qk.heads_q * qk.head_dim, qk.heads_kv * qk.head_dim
+    assert x.shape[1] >= wq + (2 if v_out is not None else 1) * wk and q_out.shape[0] == M and q_out.shape[1] >= wq and k_out.shape[1] >= wk
+    assert q_out.dtype == k_out.dtype == x.dtype and (v_out is None or (v_out.dtype == x.dtype and v_out.shape[0] == k_out.shape[0] and v_out.shape[1] >= wk))
+    assert k_out.shape[0] == M if slots is None else (slots.is_cuda and slots.is_contiguous() and slots.dtype == torch.int32 and slots.numel() == M)
+    _check(lib().dirotq_qk_norm_rope(x.data_ptr(), _DTYPES[x.dtype], M, _row_stride(x, wq + 2 * wk), qk._ref(M), q_out.data_ptr(), _row_stride(q_out, wq),
+                                     k_out.data_ptr(), _row_stride(k_out, wk), _ptr(v_out), 0 if v_out is None else _row_stride(v_out, wk), _ptr(slots),
+                                     0 if slots is None else k_out.shape[0], _stream(stream)), "dirotq_qk_norm_rope")
+
+
+def dirotq_linear_qkv(x: torch.Tensor, layer: Layer, y: torch.Tensor, workspace: torch.Tensor, qk: QkNorm, stream=None) -> None:
+    """dirotq_linear on a fused q/k/v layer, then norm and rotation of q and k in place on y."""
+    _check(lib().dirotq_linear_qkv(x.data_ptr(), x.shape[0], layer.handle, qk._ref(x.shape[0]), y.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                   _stream(stream)), "dirotq_linear_qkv")
+
+
+def dirotq_mxfp4_qkv(x: torch.Tensor, w: Mxfp4, y: torch.Tensor, workspace: torch.Tensor, qk: QkNorm, bias: torch.Tensor | None = None,
+                     scale_rule: int = MX_SCALE_FLOOR, stream=None) -> None:
+    """dirotq_mxfp4_linear on a fused q/k/v weight with norm and rotation of q and k before the result is rounded."""
+    assert x.shape[1] == w.K and tuple(y.shape) == (x.shape[0], w.rows)
+    _check_bias(bias, y)
+    _check(lib().dirotq_mxfp4_qkv(x.data_ptr(), _DTYPES[x.dtype], _row_stride(x, w.K), x.shape[0], scale_rule, w.handle, _ptr(bias), qk._ref(x.shape[0]),
+                                  y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, w.rows), workspace.data_ptr(), workspace.numel(), _stream(stream)),
+           "dirotq_mxfp4_qkv")

@@ -1,0 +1,451 @@
+// MXFP4 operands: handles, quantizer, dequantizer, plain import / export, and the entry points of the products.
+#include "mxfp4.cuh"
+#include "ptx.cuh"
+
+#include <new>
+#include <string.h>
+
+namespace dirotq {
+namespace {
+
+constexpr int kThreads = 256;
+
+// ------------------------------------------------------------------ quantizer, elements along a row
+// A unit is 256 elements of a row (two scale words).  A warp takes a unit at a time, eight elements per lane: four lanes share a block of
+// 32, so the maximum is two shuffles, a block's codes are four words side by side, a warp's codes 128 bytes.
+constexpr int kUnits = 4;  // units per warp, their loads in flight together
+
+template <typename T, bool WIDE>
+__device__ __forceinline__ void load_row8(const T* row, int k0, int K, float (&v)[8]) {
+    if (WIDE && k0 + 8 <= K) {
+        load8<T>(row + k0, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k0 + i < K ? to_f32<T>(row[k0 + i]) : 0.f;
+    }
+}
+
+template <int RULE>
+__device__ __forceinline__ uint32_t quantize8(const float (&v)[8], uint32_t byte) {
+    const float inv = mx_inverse(byte);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) w |= to_e2m1x2(v[i] * inv, v[i + 1] * inv) << (4 * i);
+    return byte == 255u ? 0u : w;
+}
+
+template <typename T, int RULE, bool WIDE>
+__global__ void __launch_bounds__(kThreads) mx_quantize_rows_kernel(const T* __restrict__ x, long long ldx, int rows, int K, int nkb, int pitch,
+                                                                    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    const int lane = threadIdx.x & 31;
+    const long long units = static_cast<long long>(rows) * nkb;
+    const long long first = (static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
+    // the previous kernel of the stream may still read the workspace this one writes, or write x
+    grid_dependency_wait();
+    grid_launch_dependents();
+    float v[kUnits][8];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const long long unit = first + u;
+        if (unit < units) {
+            const int row = static_cast<int>(unit / nkb), kb = static_cast<int>(unit % nkb);
+            load_row8<T, WIDE>(x + row * ldx, kb * 256 + lane * 8, K, v[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const long long unit = first + u;
+        if (unit >= units) break;  // (the same for the whole warp)
+        const int row = static_cast<int>(unit / nkb), kb = static_cast<int>(unit % nkb);
+        uint32_t am = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) am = max(am, __float_as_uint(v[u][i]) & 0x7fffffffu);
+        am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
+        am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
+        const int k0 = kb * 256 + lane * 8;
+        const uint32_t byte = mx_scale_byte<RULE>(am);
+        const uint32_t word = quantize8<RULE>(v[u], byte);
+        if (k0 < pitch * 2) *reinterpret_cast<uint32_t*>(codes + static_cast<size_t>(row) * pitch + k0 / 2) = word;
+        // lane 16 h gathers the bytes of blocks 4 h .. 4 h + 3 of the unit
+        uint32_t sw = byte << (8 * ((lane >> 2) & 3));
+        sw |= __shfl_xor_sync(0xffffffffu, sw, 4);
+        sw |= __shfl_xor_sync(0xffffffffu, sw, 8);
+        if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(scales + mx_scale_word(row, kb * 2 + (lane >> 4), nkb)) = sw;
+    }
+}
+
+// ------------------------------------------------------------------ quantizer, elements along a column (weights stored [K, N])
+// A block of threads takes 32 columns x 256 elements along K: a thread has one column's block of 32 in registers (the lanes of a warp read
+// consecutive columns), codes leave through shared memory so that a column's 128 bytes are written together.
+template <typename T, int RULE>
+__global__ void __launch_bounds__(kThreads) mx_quantize_cols_kernel(const T* __restrict__ x, long long ldx, int rows, int K, int nkb, int pitch,
+                                                                    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    __shared__ uint4 s_codes[32][9];  // (a row of padding: the threads of a warp write different columns' rows)
+    __shared__ __align__(16) uint8_t s_scales[32][8];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int kb = blockIdx.x % nkb;
+    const int row0 = blockIdx.x / nkb * 32;
+    const int row = row0 + lane, k0 = kb * 256 + w * 32;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    float v[32];
+    uint32_t am = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = row < rows && k0 + i < K ? to_f32<T>(x[(k0 + i) * ldx + row]) : 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) am = max(am, __float_as_uint(v[i]) & 0x7fffffffu);
+    const uint32_t byte = mx_scale_byte<RULE>(am);
+    const float inv = mx_inverse(byte);
+    uint32_t c[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) c[i >> 3] |= to_e2m1x2(v[i] * inv, v[i + 1] * inv) << (4 * (i & 7));
+    s_codes[lane][w] = byte == 255u ? make_uint4(0, 0, 0, 0) : make_uint4(c[0], c[1], c[2], c[3]);
+    s_scales[lane][w] = static_cast<uint8_t>(byte);
+    __syncthreads();
+    const int r = threadIdx.x >> 3, piece = threadIdx.x & 7;  // 32 columns x 8 pieces of 16 bytes
+    if (row0 + r < rows) {
+        const int at = kb * 128 + piece * 16;
+        if (at < pitch) *reinterpret_cast<uint4*>(codes + static_cast<size_t>(row0 + r) * pitch + at) = s_codes[r][piece];
+        if (piece < 2)
+            *reinterpret_cast<uint32_t*>(scales + mx_scale_word(row0 + r, kb * 2 + piece, nkb)) =
+                *reinterpret_cast<const uint32_t*>(&s_scales[r][piece * 4]);
+    }
+}
+
+// ------------------------------------------------------------------ dequantizer: the quantizer's units, backwards
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int K,
+                                                                 int nkb, int pitch, T* __restrict__ y, long long ldy) {
+    const int lane = threadIdx.x & 31;
+    const long long units = static_cast<long long>(rows) * nkb;
+    const long long first = (static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    uint32_t word[kUnits], sw[kUnits];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const long long unit = first + u;
+        if (unit >= units) continue;
+        const int row = static_cast<int>(unit / nkb), kb = static_cast<int>(unit % nkb);
+        const int k0 = kb * 256 + lane * 8;
+        word[u] = k0 < pitch * 2 ? *reinterpret_cast<const uint32_t*>(codes + static_cast<size_t>(row) * pitch + k0 / 2) : 0u;
+        sw[u] = *reinterpret_cast<const uint32_t*>(scales + mx_scale_word(row, kb * 2 + (lane >> 4), nkb));
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const long long unit = first + u;
+        if (unit >= units) break;
+        const int row = static_cast<int>(unit / nkb), kb = static_cast<int>(unit % nkb);
+        const int k0 = kb * 256 + lane * 8;
+        const float s = e8m0_value((sw[u] >> (8 * ((lane >> 2) & 3))) & 0xffu);
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 p = from_e2m1x2((word[u] >> (8 * i)) & 0xffu);
+            v[2 * i] = p.x * s;
+            v[2 * i + 1] = p.y * s;
+        }
+        T* out = y + row * ldy;
+        if (WIDE && k0 + 8 <= K) {
+            store8<T>(out + k0, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k0 + i < K) out[k0 + i] = from_f32<T>(v[i]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ plain form of checkpoints
+// One thread per 32-bit word of the operand's codes (and its scale byte where it starts a block); bytes behind K become zeros.
+__global__ void __launch_bounds__(kThreads) mx_import_kernel(const uint8_t* __restrict__ in_codes, const uint8_t* __restrict__ in_scales, int rows, int K,
+                                                             int nkb, int pitch, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    const int words = nkb * 32;
+    const long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
+    if (i >= static_cast<long long>(rows) * words) return;
+    const int row = static_cast<int>(i / words), w = static_cast<int>(i % words);
+    const int k0 = w * 8, kbytes = (K + 1) / 2, nblk = (K + 31) / 32;
+    uint32_t word = 0;
+    for (int b = 0; b < 4; ++b) {
+        const int k = k0 + 2 * b;
+        if (k < K) {
+            uint32_t c = in_codes[static_cast<size_t>(row) * kbytes + k / 2];
+            if (k + 1 == K) c &= 15u;
+            word |= c << (8 * b);
+        }
+    }
+    if (k0 < pitch * 2) *reinterpret_cast<uint32_t*>(codes + static_cast<size_t>(row) * pitch + k0 / 2) = word;
+    if ((w & 15) == 0) {  // the four scales of 128 elements
+        uint32_t sw = 0;
+        for (int b = 0; b < 4; ++b) {
+            const int blk = k0 / 32 + b;
+            if (blk < nblk) sw |= static_cast<uint32_t>(in_scales[static_cast<size_t>(row) * nblk + blk]) << (8 * b);
+        }
+        *reinterpret_cast<uint32_t*>(scales + mx_scale_word(row, w >> 4, nkb)) = sw;
+    }
+}
+
+__global__ void __launch_bounds__(kThreads) mx_export_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int K, int nkb,
+                                                             int pitch, uint8_t* __restrict__ out_codes, uint8_t* __restrict__ out_scales) {
+    const int kbytes = (K + 1) / 2, nblk = (K + 31) / 32;
+    const long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
+    if (i >= static_cast<long long>(rows) * kbytes) return;
+    const int row = static_cast<int>(i / kbytes), b = static_cast<int>(i % kbytes);
+    if (out_codes) out_codes[i] = codes[static_cast<size_t>(row) * pitch + b];
+    if (out_scales && (b & 15) == 0)
+        out_scales[static_cast<size_t>(row) * nblk + b / 16] = scales[mx_scale_word(row, b >> 6, nkb) + ((b >> 4) & 3)];
+}
+
+inline bool wide_rows(const void* p, long long ld, int dtype) {
+    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * static_cast<long long>(dtype_size(dtype)) % 16 == 0;
+}
+inline unsigned unit_blocks(int rows, int nkb) {
+    const long long per = (kThreads / 32) * kUnits;
+    return static_cast<unsigned>((static_cast<long long>(rows) * nkb + per - 1) / per);
+}
+inline bool fits_grid(long long blocks) { return blocks <= 0x7fffffffll; }
+
+template <typename T>
+cudaError_t quantize_t(const void* x, int layout, long long ldx, int rule, const dirotq_mxfp4* t, cudaStream_t stream) {
+    const T* in = static_cast<const T*>(x);
+    uint8_t* codes = reinterpret_cast<uint8_t*>(t->buffer);
+    uint8_t* scales = codes + t->lay.off_scales;
+    const bool floor = rule == DIROTQ_MX_SCALE_FLOOR;
+    const bool wide = wide_rows(x, ldx, sizeof(T) == 4 ? DIROTQ_DTYPE_F32 : DIROTQ_DTYPE_BF16);
+    auto kern = layout == DIROTQ_LAYOUT_KN
+                    ? (floor ? mx_quantize_cols_kernel<T, DIROTQ_MX_SCALE_FLOOR> : mx_quantize_cols_kernel<T, DIROTQ_MX_SCALE_CEIL>)
+                : wide ? (floor ? mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_FLOOR, true> : mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_CEIL, true>)
+                       : (floor ? mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_FLOOR, false> : mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_CEIL, false>);
+    const unsigned blocks = layout == DIROTQ_LAYOUT_KN ? static_cast<unsigned>((t->rows + 31) / 32) * t->lay.nkb : unit_blocks(t->rows, t->lay.nkb);
+    return launch_kernel(kern, static_cast<int>(blocks), kThreads, 0, stream, true, in, ldx, t->rows, t->K, t->lay.nkb, t->lay.pitch, codes, scales);
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+dirotq_status_t current_device(int* device) {
+    cudaError_t e = cudaGetDevice(device);
+    if (e != cudaSuccess) { set_error("cudaGetDevice", e); return DIROTQ_ERR_CUDA; }
+    int major = 0;
+    e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *device);
+    if (e != cudaSuccess) { set_error("cudaDeviceGetAttribute", e); return DIROTQ_ERR_CUDA; }
+    return major == 10 ? DIROTQ_OK : DIROTQ_ERR_ARCH;
+}
+
+dirotq_status_t check_shape(int rows, int K) {
+    if (rows < 1 || K < 1) return DIROTQ_ERR_INVALID_ARG;
+    if (rows > (1 << 24) || K > (1 << 20)) return DIROTQ_ERR_UNSUPPORTED_SHAPE;
+    // every kernel's grid: at most one block per 256 bytes of codes
+    return fits_grid(static_cast<long long>(rows) * ((K + 255) / 256)) ? DIROTQ_OK : DIROTQ_ERR_UNSUPPORTED_SHAPE;
+}
+
+dirotq_status_t check_operand(const dirotq_mxfp4* t) {
+    if (!mx_valid(t)) return DIROTQ_ERR_INVALID_ARG;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return DIROTQ_ERR_CUDA;
+    return dev == t->device ? DIROTQ_OK : DIROTQ_ERR_INVALID_ARG;
+}
+
+dirotq_status_t done(const char* what, cudaError_t e) {
+    if (e == cudaSuccess) return DIROTQ_OK;
+    set_error(what, e);
+    return DIROTQ_ERR_CUDA;
+}
+
+constexpr size_t kStatusBytes = 256;
+
+dirotq_status_t check_product(const dirotq_mxfp4* a_or_null, const dirotq_mxfp4* b, const void* bias, const void* y, int y_dtype, long long ldy) {
+    if (!mx_valid(b) || (a_or_null && !mx_valid(a_or_null)) || !y || !dtype_is_16(y_dtype)) return DIROTQ_ERR_INVALID_ARG;
+    if (a_or_null && a_or_null->K != b->K) return DIROTQ_ERR_INVALID_ARG;
+    if (ldy < b->rows) return DIROTQ_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(y) & 1u) != 0 || (reinterpret_cast<uintptr_t>(bias) & 1u) != 0) return DIROTQ_ERR_INVALID_ARG;
+    return DIROTQ_OK;
+}
+
+dirotq_status_t linear(const void* x, int x_dtype, long long ldx, int M, int scale_rule, const dirotq_mxfp4* w, const void* bias,
+                       const dirotq_qk_t* qk, void* y, int y_dtype, long long ldy, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+    dirotq_status_t st = check_product(nullptr, w, bias, y, y_dtype, ldy);
+    if (st != DIROTQ_OK) return st;
+    if (!x || !dtype_ok(x_dtype) || (scale_rule != DIROTQ_MX_SCALE_FLOOR && scale_rule != DIROTQ_MX_SCALE_CEIL)) return DIROTQ_ERR_INVALID_ARG;
+    if (ldx < w->K || reinterpret_cast<uintptr_t>(x) % dtype_size(x_dtype) != 0) return DIROTQ_ERR_INVALID_ARG;
+    st = check_shape(M, w->K);
+    if (st != DIROTQ_OK) return st;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & (kAlign - 1)) != 0) return DIROTQ_ERR_INVALID_ARG;
+    if (workspace_bytes < kAlign + make_mx_layout(M, w->K).total) return DIROTQ_ERR_BUFFER_TOO_SMALL;
+    if (qk) {
+        st = qk_check(qk, M);
+        if (st != DIROTQ_OK) return st;
+        if (static_cast<long long>(qk->heads_q + 2ll * qk->heads_kv) * qk->head_dim != w->rows) return DIROTQ_ERR_INVALID_ARG;
+        if ((qk->head_dim != 64 && qk->head_dim != 128) || (qk->rot_dim != 0 && qk->rot_dim != qk->head_dim)) return DIROTQ_ERR_UNSUPPORTED_SHAPE;
+    }
+    st = check_operand(w);
+    if (st != DIROTQ_OK) return st;
+    dirotq_mxfp4 a;
+    st = mx_setup(&a, M, w->K, static_cast<char*>(workspace) + kAlign, w->device);
+    if (st != DIROTQ_OK) return st;
+    st = done("dirotq_mxfp4_linear", launch_mx_quantize(x, x_dtype, DIROTQ_LAYOUT_NK, ldx, scale_rule, &a, stream));
+    if (st != DIROTQ_OK) return st;
+    const MxGemmArgs ga = {&a, w, bias, y, y_dtype, ldy, static_cast<int*>(workspace), true, qk};
+    return launch_mx_gemm(ga, stream);
+}
+
+}  // namespace
+
+bool mx_valid(const dirotq_mxfp4* t) { return t != nullptr && t->magic == kMxMagic; }
+
+dirotq_status_t mx_setup(dirotq_mxfp4* t, int rows, int K, void* buffer, int device) {
+    memset(t, 0, sizeof *t);
+    t->magic = kMxMagic;
+    t->device = device;
+    t->rows = rows;
+    t->K = K;
+    t->lay = make_mx_layout(rows, K);
+    t->buffer = static_cast<char*>(buffer);
+    t->box = box_rows(rows);
+    return encode_tmap_2d(&t->tmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, buffer, (uint64_t)t->lay.pitch, (uint64_t)rows, (uint64_t)t->lay.pitch, 128,
+                          t->box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+cudaError_t launch_mx_quantize(const void* x, int x_dtype, int x_layout, long long ldx, int scale_rule, const dirotq_mxfp4* t, cudaStream_t stream) {
+    switch (x_dtype) {
+        case DIROTQ_DTYPE_F32: return quantize_t<float>(x, x_layout, ldx, scale_rule, t, stream);
+        case DIROTQ_DTYPE_BF16: return quantize_t<__nv_bfloat16>(x, x_layout, ldx, scale_rule, t, stream);
+        default: return quantize_t<__half>(x, x_layout, ldx, scale_rule, t, stream);
+    }
+}
+
+}  // namespace dirotq
+
+using namespace dirotq;
+
+extern "C" {
+
+dirotq_status_t dirotq_mxfp4_bytes(int rows, int K, size_t* bytes) {
+    if (!bytes) return DIROTQ_ERR_INVALID_ARG;
+    const dirotq_status_t st = check_shape(rows, K);
+    if (st != DIROTQ_OK) return st;
+    *bytes = make_mx_layout(rows, K).total;
+    return DIROTQ_OK;
+}
+
+dirotq_status_t dirotq_mxfp4_create(int rows, int K, void* buffer, size_t buffer_bytes, dirotq_mxfp4_t** out) {
+    if (!buffer || !out || (reinterpret_cast<uintptr_t>(buffer) & (kAlign - 1)) != 0) return DIROTQ_ERR_INVALID_ARG;
+    dirotq_status_t st = check_shape(rows, K);
+    if (st != DIROTQ_OK) return st;
+    if (buffer_bytes < make_mx_layout(rows, K).total) return DIROTQ_ERR_BUFFER_TOO_SMALL;
+    int dev = 0;
+    st = current_device(&dev);
+    if (st != DIROTQ_OK) return st;
+    dirotq_mxfp4* t = new (std::nothrow) dirotq_mxfp4;
+    if (!t) return DIROTQ_ERR_INVALID_ARG;
+    st = mx_setup(t, rows, K, buffer, dev);
+    if (st != DIROTQ_OK) {
+        delete t;
+        return st;
+    }
+    *out = t;
+    return DIROTQ_OK;
+}
+
+dirotq_status_t dirotq_mxfp4_destroy(dirotq_mxfp4_t* t) {
+    if (!mx_valid(t)) return DIROTQ_ERR_INVALID_ARG;
+    t->magic = 0;
+    delete t;
+    return DIROTQ_OK;
+}
+
+dirotq_status_t dirotq_mxfp4_info(const dirotq_mxfp4_t* t, int* rows, int* K) {
+    if (!mx_valid(t)) return DIROTQ_ERR_INVALID_ARG;
+    if (rows) *rows = t->rows;
+    if (K) *K = t->K;
+    return DIROTQ_OK;
+}
+
+dirotq_status_t dirotq_mxfp4_quantize(const void* x, int x_dtype, int x_layout, long long ldx, int scale_rule, const dirotq_mxfp4_t* out,
+                                      dirotq_stream_t stream) {
+    if (!mx_valid(out) || !x || !dtype_ok(x_dtype) || (x_layout != DIROTQ_LAYOUT_NK && x_layout != DIROTQ_LAYOUT_KN))
+        return DIROTQ_ERR_INVALID_ARG;
+    if (scale_rule != DIROTQ_MX_SCALE_FLOOR && scale_rule != DIROTQ_MX_SCALE_CEIL) return DIROTQ_ERR_INVALID_ARG;
+    if (ldx < (x_layout == DIROTQ_LAYOUT_NK ? out->K : out->rows) || reinterpret_cast<uintptr_t>(x) % dtype_size(x_dtype) != 0)
+        return DIROTQ_ERR_INVALID_ARG;
+    const dirotq_status_t st = check_operand(out);
+    if (st != DIROTQ_OK) return st;
+    return done("dirotq_mxfp4_quantize", launch_mx_quantize(x, x_dtype, x_layout, ldx, scale_rule, out, static_cast<cudaStream_t>(stream)));
+}
+
+dirotq_status_t dirotq_mxfp4_dequantize(const dirotq_mxfp4_t* t, void* y, int y_dtype, long long ldy, dirotq_stream_t stream) {
+    if (!mx_valid(t) || !y || !dtype_ok(y_dtype) || ldy < t->K || reinterpret_cast<uintptr_t>(y) % dtype_size(y_dtype) != 0)
+        return DIROTQ_ERR_INVALID_ARG;
+    const dirotq_status_t st = check_operand(t);
+    if (st != DIROTQ_OK) return st;
+    const uint8_t* codes = reinterpret_cast<const uint8_t*>(t->buffer);
+    const uint8_t* scales = codes + t->lay.off_scales;
+    const bool wide = wide_rows(y, ldy, y_dtype);
+    const int blocks = static_cast<int>(unit_blocks(t->rows, t->lay.nkb));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    auto go = [&](auto* out) {
+        using T = std::remove_pointer_t<decltype(out)>;
+        return launch_kernel(wide ? mx_dequantize_kernel<T, true> : mx_dequantize_kernel<T, false>, blocks, kThreads, 0, s, true, codes, scales, t->rows,
+                             t->K, t->lay.nkb, t->lay.pitch, out, ldy);
+    };
+    return done("dirotq_mxfp4_dequantize", y_dtype == DIROTQ_DTYPE_F32    ? go(static_cast<float*>(y))
+                                           : y_dtype == DIROTQ_DTYPE_BF16 ? go(static_cast<__nv_bfloat16*>(y))
+                                                                          : go(static_cast<__half*>(y)));
+}
+
+dirotq_status_t dirotq_mxfp4_import(const uint8_t* codes, const uint8_t* scales, const dirotq_mxfp4_t* out, dirotq_stream_t stream) {
+    if (!mx_valid(out) || !codes || !scales) return DIROTQ_ERR_INVALID_ARG;
+    const dirotq_status_t st = check_operand(out);
+    if (st != DIROTQ_OK) return st;
+    uint8_t* to = reinterpret_cast<uint8_t*>(out->buffer);
+    const long long words = static_cast<long long>(out->rows) * out->lay.nkb * 32;
+    return done("dirotq_mxfp4_import",
+                launch_kernel(mx_import_kernel, static_cast<int>((words + kThreads - 1) / kThreads), kThreads, 0, static_cast<cudaStream_t>(stream), false,
+                              codes, scales, out->rows, out->K, out->lay.nkb, out->lay.pitch, to, to + out->lay.off_scales));
+}
+
+dirotq_status_t dirotq_mxfp4_export(const dirotq_mxfp4_t* t, uint8_t* codes, uint8_t* scales, dirotq_stream_t stream) {
+    if (!mx_valid(t)) return DIROTQ_ERR_INVALID_ARG;
+    const dirotq_status_t st = check_operand(t);
+    if (st != DIROTQ_OK) return st;
+    const uint8_t* from = reinterpret_cast<const uint8_t*>(t->buffer);
+    const long long n = static_cast<long long>(t->rows) * ((t->K + 1) / 2);
+    return done("dirotq_mxfp4_export",
+                launch_kernel(mx_export_kernel, static_cast<int>((n + kThreads - 1) / kThreads), kThreads, 0, static_cast<cudaStream_t>(stream), false, from,
+                              from + t->lay.off_scales, t->rows, t->K, t->lay.nkb, t->lay.pitch, codes, scales));
+}
+
+dirotq_status_t dirotq_mxfp4_workspace_bytes(int M, int K, size_t* bytes) {
+    if (!bytes) return DIROTQ_ERR_INVALID_ARG;
+    const dirotq_status_t st = check_shape(M, K);
+    if (st != DIROTQ_OK) return st;
+    *bytes = kAlign + make_mx_layout(M, K).total;
+    return DIROTQ_OK;
+}
+
+dirotq_status_t dirotq_mxfp4_gemm(const dirotq_mxfp4_t* a, const dirotq_mxfp4_t* b, const void* bias, void* y, int y_dtype, long long ldy,
+                                  void* workspace, size_t workspace_bytes, dirotq_stream_t stream) {
+    if (!a) return DIROTQ_ERR_INVALID_ARG;
+    dirotq_status_t st = check_product(a, b, bias, y, y_dtype, ldy);
+    if (st != DIROTQ_OK) return st;
+    if (!workspace || !aligned16(workspace)) return DIROTQ_ERR_INVALID_ARG;
+    if (workspace_bytes < kStatusBytes) return DIROTQ_ERR_BUFFER_TOO_SMALL;
+    st = check_operand(a);
+    if (st == DIROTQ_OK) st = check_operand(b);
+    if (st != DIROTQ_OK) return st;
+    const MxGemmArgs ga = {a, b, bias, y, y_dtype, ldy, static_cast<int*>(workspace), false, nullptr};
+    return launch_mx_gemm(ga, static_cast<cudaStream_t>(stream));
+}
+
+dirotq_status_t dirotq_mxfp4_linear(const void* x, int x_dtype, long long ldx, int M, int scale_rule, const dirotq_mxfp4_t* w, const void* bias,
+                                    void* y, int y_dtype, long long ldy, void* workspace, size_t workspace_bytes, dirotq_stream_t stream) {
+    return linear(x, x_dtype, ldx, M, scale_rule, w, bias, nullptr, y, y_dtype, ldy, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+dirotq_status_t dirotq_mxfp4_qkv(const void* x, int x_dtype, long long ldx, int M, int scale_rule, const dirotq_mxfp4_t* w, const void* bias,
+                                 const dirotq_qk_t* qk, void* y, int y_dtype, long long ldy, void* workspace, size_t workspace_bytes,
+                                 dirotq_stream_t stream) {
+    if (!qk) return DIROTQ_ERR_INVALID_ARG;
+    return linear(x, x_dtype, ldx, M, scale_rule, w, bias, qk, y, y_dtype, ldy, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
