@@ -34,18 +34,18 @@ struct MxPlan {
     static constexpr int NB = BN / 128;             // 128-column blocks of a tile
     static constexpr int B_BYTES = 128 * 128;       // this CTA's rows of b: the tile's (single) or half of them (pair)
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + (1 + NB) * ATOMS;  // 34 / 35 KB
-    static constexpr int STAGES = 5;
+    static constexpr int STAGES = 6;
     static constexpr int ACC_BUFS = PAIR ? 1 : 2;
     static constexpr int BAR_OFFSET = STAGES * STAGE_BYTES;
     static constexpr int BIAS_OFFSET = BAR_OFFSET + 256;                         // per warpgroup two buffers of 128 values
     static constexpr int HEADW_OFFSET = BIAS_OFFSET + 4 * 128 * 4;               // q and k weights of a head, 128 values each
-    static constexpr int STORE_OFFSET = (HEADW_OFFSET + 2 * 128 * 4 + 1023) / 1024 * 1024;  // 32 rows x 128 bytes per epilogue warp
-    static constexpr int SMEM_BYTES = STORE_OFFSET + NUM_EPI_WARPS * 4096 + 1024;
+    static constexpr int EDGE_OFFSET = HEADW_OFFSET + 2 * 128 * 4;               // 8 rows x 128 bytes per epilogue warp: rows of y of any alignment
+    static constexpr int SMEM_BYTES = EDGE_OFFSET + NUM_EPI_WARPS * 1024 + 1024;
     static constexpr int TMEM_SF = ACC_BUFS * BN;   // columns of the scales: per stage 8 for a, 8 per 128 columns
     static constexpr int SF_COLS = 8 * (1 + NB);
     static_assert(PAIR ? BN == 256 : BN == 128, "plans");
     static_assert(TMEM_SF + STAGES * SF_COLS <= 512, "tensor memory plan");
-    static_assert(8 * (4 * STAGES + 4) <= 192, "barriers end below the words at +192");
+    static_assert(8 * ((PAIR ? 4 : 3) * STAGES + 4) <= 240, "barriers end below the words at +240");
     static_assert(SMEM_BYTES <= 232448, "shared memory plan");
     static_assert(STAGE_BYTES % 1024 == 0, "operand tiles must stay 1024-byte aligned");
 };
@@ -60,7 +60,7 @@ struct MxKernelParams {
     long long ldy;
     int* status;
     int f16;               // y and bias are fp16 (else bf16)
-    int tma_out;           // rows of y may be written by TMA stores
+    int wide_out;          // rows of y are 16-byte aligned
     int early;             // b may be read while the previous kernel runs
     // norm and rotation of q and k
     int q_cols, k_end;     // columns [0, q_cols) are q, [q_cols, k_end) are k
@@ -73,6 +73,7 @@ struct MxKernelParams {
     const float* cos_table;
     const float* sin_table;
     long long ld_table;
+    int wide_table;        // rows of both tables are 16-byte aligned
     int num_positions;
     const int32_t* positions;
 };
@@ -140,8 +141,9 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, int f16) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// A barrier of the 128 threads of epilogue warpgroup `g` that makes them agree: true if any of them brings true.
-__device__ __forceinline__ bool group_any(int g, bool mine) {
+// Named barrier ID of the 128 threads of an epilogue warpgroup that makes them agree: true if any of them brings true.
+template <int ID>
+__device__ __forceinline__ bool group_any(bool mine) {
     uint32_t any;
     asm volatile(
         "{\n\t"
@@ -151,50 +153,122 @@ __device__ __forceinline__ bool group_any(int g, bool mine) {
         "selp.u32 %0, 1, 0, pout;\n\t"
         "}\n"
         : "=r"(any)
-        : "r"(static_cast<uint32_t>(mine)), "r"(1 + g)
+        : "r"(static_cast<uint32_t>(mine)), "n"(ID)
         : "memory");
     return any != 0;
 }
 
-// Norm and rotation of the D elements of one head, in the registers of one thread.
-template <int D>
-__device__ __forceinline__ void head_norm_rope(float* v, const float* w, const MxKernelParams& p, const float* cs, const float* sn) {
-    if (p.norm) {
-        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+// 16 tensor-memory lanes x 256 bits, eight times along the columns (64 columns): register 4 j + 2 h + e of lane l holds row l / 4 + 8 h and
+// column 8 j + 2 (l % 4) + e.
+__device__ __forceinline__ void tmem_ld_16x256b_x8(uint32_t taddr, uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(taddr)
+        : "memory");
+}
+
+// Within four consecutive lanes: lane t's word k becomes lane k's word t.
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4], int t) {
+    const bool odd = (t & 1) != 0, upper = (t & 2) != 0;
 #pragma unroll
-        for (int i = 0; i < D; i += 4) {
-            s0 = fmaf(v[i], v[i], s0);
-            s1 = fmaf(v[i + 1], v[i + 1], s1);
-            s2 = fmaf(v[i + 2], v[i + 2], s2);
-            s3 = fmaf(v[i + 3], v[i + 3], s3);
-        }
-        const float r = rsqrtf(((s0 + s1) + (s2 + s3)) * p.inv_dim + p.eps);
+    for (int k = 0; k < 4; k += 2) {
+        const uint32_t x = __shfl_xor_sync(0xffffffffu, odd ? w[k] : w[k + 1], 1);
+        if (odd) w[k] = x;
+        else w[k + 1] = x;
+    }
 #pragma unroll
-        for (int i = 0; i < D; i += 4) {
-            const float4 wv = *reinterpret_cast<const float4*>(w + i);
-            v[i] *= r * wv.x; v[i + 1] *= r * wv.y; v[i + 2] *= r * wv.z; v[i + 3] *= r * wv.w;
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t x = __shfl_xor_sync(0xffffffffu, upper ? w[k] : w[k + 2], 2);
+        if (upper) w[k] = x;
+        else w[k + 2] = x;
+    }
+}
+
+// Cosines and sines of four consecutive angles (`wide`: 16-byte aligned).
+__device__ __forceinline__ void load_angles(const float* cs, const float* sn, int wide, float (&c)[4], float (&s)[4]) {
+    if (wide) {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(cs)), b = __ldg(reinterpret_cast<const float4*>(sn));
+        c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w;
+        s[0] = b.x; s[1] = b.y; s[2] = b.z; s[3] = b.w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            c[k] = __ldg(cs + k);
+            s[k] = __ldg(sn + k);
         }
     }
-    if (p.rope == DIROTQ_ROPE_PAIRS) {
+}
+
+// Norm and rotation of one head of a row, held by four lanes: lane t has elements 32 m + 8 t + e of its R * 32.  `turned`: false for rows that keep
+// what the projection made them (all lanes take part in the sum).
+template <int R>
+__device__ __forceinline__ void head_norm_rope(float (*v)[8], bool turned, const float* w, int t, int pos, const MxKernelParams& p) {
+    if (p.norm) {
+        float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-        for (int i = 0; i < D / 2; ++i) {
-            const float c = __ldg(cs + i), s = __ldg(sn + i), a = v[2 * i], b = v[2 * i + 1];
-            v[2 * i] = a * c - b * s;
-            v[2 * i + 1] = a * s + b * c;
-        }
-    } else if (p.rope == DIROTQ_ROPE_HALVES) {
+        for (int m = 0; m < R; ++m)
 #pragma unroll
-        for (int i = 0; i < D / 2; ++i) {
-            const float c = __ldg(cs + i), s = __ldg(sn + i), a = v[i], b = v[i + D / 2];
-            v[i] = a * c - b * s;
-            v[i + D / 2] = a * s + b * c;
+            for (int e = 0; e < 8; e += 2) {
+                s0 = fmaf(v[m][e], v[m][e], s0);
+                s1 = fmaf(v[m][e + 1], v[m][e + 1], s1);
+            }
+        s0 += s1;
+        s0 += __shfl_xor_sync(0xffffffffu, s0, 1);
+        s0 += __shfl_xor_sync(0xffffffffu, s0, 2);
+        if (!turned) return;
+        const float r = rsqrtf(s0 * p.inv_dim + p.eps);
+#pragma unroll
+        for (int m = 0; m < R; ++m)
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+                const float4 g = *reinterpret_cast<const float4*>(w + 32 * m + 8 * t + e);
+                v[m][e] *= r * g.x;
+                v[m][e + 1] *= r * g.y;
+                v[m][e + 2] *= r * g.z;
+                v[m][e + 3] *= r * g.w;
+            }
+    }
+    if (!turned) return;
+    const float* cs = p.cos_table + static_cast<long long>(pos) * p.ld_table;
+    const float* sn = p.sin_table + static_cast<long long>(pos) * p.ld_table;
+    if (p.rope == DIROTQ_ROPE_PAIRS) {  // angles 16 m + 4 t ..
+#pragma unroll
+        for (int m = 0; m < R; ++m) {
+            float c[4], s[4];
+            load_angles(cs + 16 * m + 4 * t, sn + 16 * m + 4 * t, p.wide_table, c, s);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float a = v[m][2 * k], b = v[m][2 * k + 1];
+                v[m][2 * k] = a * c[k] - b * s[k];
+                v[m][2 * k + 1] = a * s[k] + b * c[k];
+            }
         }
+    } else if (p.rope == DIROTQ_ROPE_HALVES) {  // element i and i + R * 16: the same lane, R / 2 runs further on
+#pragma unroll
+        for (int m = 0; m < R / 2; ++m)
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+                float c[4], s[4];
+                load_angles(cs + 32 * m + 8 * t + e, sn + 32 * m + 8 * t + e, p.wide_table, c, s);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float a = v[m][e + k], b = v[m + R / 2][e + k];
+                    v[m][e + k] = a * c[k] - b * s[k];
+                    v[m + R / 2][e + k] = a * s[k] + b * c[k];
+                }
+            }
     }
 }
 
 template <int BN, bool PAIR, bool QKV>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
-mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ CUtensorMap tmap_y,
+mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                const __grid_constant__ MxKernelParams p) {
     using P = MxPlan<BN, PAIR>;
     constexpr int NB = P::NB, STAGES = P::STAGES, ACC_BUFS = P::ACC_BUFS, STAGE_BYTES = P::STAGE_BYTES;
@@ -205,11 +279,12 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
     auto full_bar = [&](int s) { return bar_base + 8u * s; };
     auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
     auto sfready_bar = [&](int s) { return bar_base + 8u * (2 * STAGES + s); };
-    auto peer_bar = [&](int s) { return bar_base + 8u * (3 * STAGES + s); };  // pairs, leader: the other CTA's stage has landed
-    auto tfull_bar = [&](int a) { return bar_base + 8u * (4 * STAGES + a); };
-    auto tempty_bar = [&](int a) { return bar_base + 8u * (4 * STAGES + 2 + a); };
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_gen + P::BAR_OFFSET + 192);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + P::BAR_OFFSET + 196);
+    auto tfull_bar = [&](int a) { return bar_base + 8u * (3 * STAGES + a); };
+    auto tempty_bar = [&](int a) { return bar_base + 8u * (3 * STAGES + 2 + a); };
+    auto peer_bar = [&](int s) { return bar_base + 8u * (3 * STAGES + 4 + s); };  // pairs, leader: the other CTA's stage has landed
+    const uint32_t drain_bar = bar_base + 248u;  // see umma_drain
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_gen + P::BAR_OFFSET + 240);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + P::BAR_OFFSET + 244);
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
@@ -225,18 +300,17 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             mbar_init(full_bar(s), 1);
             mbar_init(empty_bar(s), 1);
             mbar_init(sfready_bar(s), 2);  // one arrival per copier warp
-            mbar_init(peer_bar(s), 1);
+            if constexpr (PAIR) mbar_init(peer_bar(s), 1);
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(tfull_bar(a), 1);
             mbar_init(tempty_bar(a), PAIR ? 2 * NUM_EPI_WARPS * 32 : NUM_EPI_WARPS * 32 / 2);
         }
-        mbar_init(bar_base + 200u, 1);  // spare: see umma_drain
+        mbar_init(drain_bar, 1);
         *abort_flag = 0;
         fence_mbar_init();
         tma_prefetch_desc(&tmap_a);
         tma_prefetch_desc(&tmap_b);
-        if (p.tma_out) tma_prefetch_desc(&tmap_y);
     }
     if (warp == 1) {
         if constexpr (PAIR) {
@@ -255,6 +329,10 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
     grid_dependency_wait();  // everything above touched only this CTA's own shared and tensor memory
     grid_launch_dependents();
 
+    if (warp < 4) {
+    // With the norm and rotation an epilogue thread holds 32 values in transit beside the 128 it has read: 72 and 208 registers a thread
+    // (128 * 72 + 256 * 208 of the 384 * 168 at launch)
+    if constexpr (QKV) reg_dealloc<72>();
     if (warp == 0) {
         // ------------------------------------------------------------ producer
         RingPos<STAGES> at;
@@ -319,7 +397,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
                 }
             }
         }
-    } else if (warp < 4) {
+    } else {
         // ------------------------------------------------------------ scale copiers
         RingPos<STAGES> at;
         bool ok = true;
@@ -353,11 +431,19 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
                 else umma_commit(sfready_bar(s));
             }
         }
+    }
     } else {
         // ------------------------------------------------------------ epilogue
+        if constexpr (QKV) reg_alloc<208>();
         // warp % 4 selects the quadrant of tensor-memory lanes (32 rows); a warpgroup has 128 columns: half of a pair's tile, or the whole of
-        // every second 128-column tile.  A thread reads its row's 128 columns and hands the accumulator back before it converts them.
+        // every second 128-column tile.  A warp reads its 32 x 128 values and hands the accumulator back before it converts them.
+        //
+        // Loads of 16 lanes x 256 bits leave lane l with columns 8 J + 2 t, + 1 (t = l % 4, J = 0..15) of rows l / 4 + 8 i (i = 0..3): exchanged within
+        // the four lanes of a row (transpose4), each lane has four runs of 8 consecutive columns, 32 m + 8 t, of its four rows, 64 bytes of a
+        // row side by side in a store.  (Through shared memory and TMA stores instead: the same time at K = 12288, and 32 KB that hold a
+        // stage of operands here.)
         const int q = warp & 3, group = (warp - 4) >> 2, gt = threadIdx.x & 127;
+        const int t = lane & 3, r4 = lane >> 2;
         float* s_hw = reinterpret_cast<float*>(smem_gen + P::HEADW_OFFSET);
         if constexpr (QKV) {  // (both warpgroups write the same values; each reads behind its own barrier below)
             const int i = gt & ((1 << p.head_shift) - 1);
@@ -366,7 +452,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
         }
         uint32_t tcount = PAIR ? 0 : group;
         for (int tile = tile_first + (PAIR ? 0 : group * tile_step); tile < num_tiles; tile += PAIR ? tile_step : 2 * tile_step, tcount += PAIR ? 1 : 2) {
-            const int m0 = (tile % num_m_blocks) * TILE_ROWS + (PAIR ? static_cast<int>(cta_rank) * BM : 0);
+            const int row0 = (tile % num_m_blocks) * TILE_ROWS + (PAIR ? static_cast<int>(cta_rank) * BM : 0) + q * 32;
             const int n0 = (tile / num_m_blocks) * BN + (PAIR ? group * 128 : 0);
             const uint32_t acc = tcount % ACC_BUFS, use = tcount / ACC_BUFS;
             // the bias of these columns goes to shared memory while the tile's MMAs run (two buffers: a warp can be a tile ahead); the
@@ -374,88 +460,112 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             float* s_b = reinterpret_cast<float*>(smem_gen + P::BIAS_OFFSET) + (group * 2 + (use & 1)) * 128;
             s_b[gt] = p.bias != nullptr && n0 + gt < p.N ? load_16(p.bias, n0 + gt, p.f16) : 0.f;
             const bool failed = !mbar_wait(tfull_bar(acc), use & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
-            if (group_any(group, failed)) break;
+            if (group == 0 ? group_any<1>(failed) : group_any<2>(failed)) break;
             tc_fence_after_sync();
             const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * BN + (PAIR ? group * 128 : 0);
-            uint32_t raw[4][32];
+            uint32_t raw[2][2][32];  // [rows 16 h ..][columns 64 c ..][4 j + 2 (row + 8) + (column + 1)], J = 8 c + j
+            const bool stored = row0 < p.M && n0 < p.N;  // (uniform in the warp)
+            if (stored) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(taddr + c * 32, raw[c]);
-            tmem_ld_wait();
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld_fence(raw[c]);
+                    for (int c = 0; c < 2; ++c) tmem_ld_16x256b_x8(taddr + (static_cast<uint32_t>(16 * h) << 16) + c * 64, raw[h][c]);
+                tmem_ld_wait();
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) tmem_ld_fence(raw[h][c]);
+            }
             tc_fence_before_sync();
             if constexpr (PAIR) mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));  // the leader's barrier
             else mbar_arrive(tempty_bar(acc));
-            const int row0 = m0 + q * 32;
-            float* v = reinterpret_cast<float*>(&raw[0][0]);
+            if (!stored) continue;
 #pragma unroll
-            for (int i = 0; i < 128; i += 4) {
-                const float4 b = *reinterpret_cast<const float4*>(s_b + i);
-                v[i] += b.x; v[i + 1] += b.y; v[i + 2] += b.z; v[i + 3] += b.w;
-            }
-            if constexpr (QKV) {
-                // columns are whole heads: 128 is one head of 128 or two of 64
-                const int row = row0 + lane;
-                int pos = row;
-                if (p.positions != nullptr && row < p.M) pos = __ldg(p.positions + row);
-                if (n0 < p.k_end && row < p.M && (p.rope == DIROTQ_ROPE_NONE || (pos >= 0 && pos < p.num_positions))) {
-                    const float* cs = p.cos_table + static_cast<long long>(pos) * p.ld_table;
-                    const float* sn = p.sin_table + static_cast<long long>(pos) * p.ld_table;
-                    if (p.head_shift == 7) {
-                        head_norm_rope<128>(v, n0 < p.q_cols ? s_hw : s_hw + 128, p, cs, sn);
-                    } else {
-                        head_norm_rope<64>(v, n0 < p.q_cols ? s_hw : s_hw + 128, p, cs, sn);
-                        if (n0 + 64 < p.k_end) head_norm_rope<64>(v + 64, n0 + 64 < p.q_cols ? s_hw : s_hw + 128, p, cs, sn);
-                    }
-                }
-            }
-            // outputs leave through a staging tile per warp, 64 columns at a time (128-byte swizzle: a quarter-warp's pieces fall into different
-            // banks): a TMA store writes whole lines and clips at M and N; what it cannot address is written by the lanes
-            const uint32_t sbuf = smem_base + P::STORE_OFFSET + static_cast<uint32_t>(warp - 4) * 4096u;
+            for (int i = 0; i < 4; ++i) {
+                if (row0 + 8 * i >= p.M) break;
+                const int row = row0 + 8 * i + r4;
+                uint4 out[4];
+                if (QKV && n0 < p.k_end) {
+                    float v[4][8];  // columns 32 m + 8 t + e
 #pragma unroll
-            for (int cc = 0; cc < 2; ++cc) {
-                if (lane == 0) bulk_wait_group_read_all();  // the staging tile's previous contents have been read
-                __syncwarp();
+                    for (int m = 0; m < 4; ++m) {
+                        uint32_t lo[4], hi[4];
 #pragma unroll
-                for (int p8 = 0; p8 < 8; ++p8) {
-                    const float* e = v + cc * 64 + p8 * 8;
-                    const uint32_t dst = sbuf + static_cast<uint32_t>(lane) * 128u + (static_cast<uint32_t>(p8 ^ (lane & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(pack2(e[0], e[1], p.f16)), "r"(pack2(e[2], e[3], p.f16)),
-                                 "r"(pack2(e[4], e[5], p.f16)), "r"(pack2(e[6], e[7], p.f16))
-                                 : "memory");
-                }
-                const int col0 = n0 + cc * 64;
-                // (a TMA store writes 16-byte pieces whole: a ragged last one is left to the lanes)
-                if (p.tma_out && (col0 + 64 <= p.N || (p.N & 7) == 0)) {
-                    fence_proxy_async_smem();  // these writes -> visible to the copy engine
-                    __syncwarp();
-                    if (lane == 0 && row0 < p.M && col0 < p.N) {
-                        tma_store_2d(&tmap_y, sbuf, col0, row0);
-                        bulk_commit_group();
-                    }
-                } else {
-                    __syncwarp();
-                    const int rows = min(32, p.M - row0), cols = min(64, p.N - col0);
-                    for (int r = 0; r < rows; ++r) {
-                        uint16_t* out = reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row0 + r) * p.ldy + col0;
+                        for (int k = 0; k < 4; ++k) {
+                            lo[k] = raw[i >> 1][m >> 1][16 * (m & 1) + 4 * k + 2 * (i & 1)];
+                            hi[k] = raw[i >> 1][m >> 1][16 * (m & 1) + 4 * k + 2 * (i & 1) + 1];
+                        }
+                        transpose4(lo, t);
+                        transpose4(hi, t);
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int c = lane + 32 * h;
-                            uint16_t e;
-                            const uint32_t src = sbuf + static_cast<uint32_t>(r) * 128u + (static_cast<uint32_t>((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2;
-                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(e) : "r"(src) : "memory");
-                            if (c < cols) out[c] = e;
+                        for (int k = 0; k < 4; ++k) {
+                            const float2 b = *reinterpret_cast<const float2*>(s_b + 32 * m + 8 * t + 2 * k);
+                            v[m][2 * k] = __uint_as_float(lo[k]) + b.x;
+                            v[m][2 * k + 1] = __uint_as_float(hi[k]) + b.y;
                         }
                     }
-                    __syncwarp();
+                    int pos = row;
+                    if (p.positions != nullptr && row < p.M) pos = __ldg(p.positions + row);
+                    const bool turned = row < p.M && (p.rope == DIROTQ_ROPE_NONE || (pos >= 0 && pos < p.num_positions));
+                    if (!turned) pos = 0;
+                    if (p.head_shift == 7) head_norm_rope<4>(v, turned, s_hw + (n0 < p.q_cols ? 0 : 128), t, pos, p);
+                    else {
+                        head_norm_rope<2>(v, turned, s_hw + (n0 < p.q_cols ? 0 : 128), t, pos, p);
+                        head_norm_rope<2>(v + 2, turned && n0 + 64 < p.k_end, s_hw + (n0 + 64 < p.q_cols ? 0 : 128), t, pos, p);
+                    }
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+                        out[m] = make_uint4(pack2(v[m][0], v[m][1], p.f16), pack2(v[m][2], v[m][3], p.f16), pack2(v[m][4], v[m][5], p.f16),
+                                            pack2(v[m][6], v[m][7], p.f16));
+                } else {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float2 b = *reinterpret_cast<const float2*>(s_b + 32 * m + 8 * k + 2 * t);
+                            w[k] = pack2(__uint_as_float(raw[i >> 1][m >> 1][16 * (m & 1) + 4 * k + 2 * (i & 1)]) + b.x,
+                                         __uint_as_float(raw[i >> 1][m >> 1][16 * (m & 1) + 4 * k + 2 * (i & 1) + 1]) + b.y, p.f16);
+                        }
+                        transpose4(w, t);
+                        out[m] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+                uint16_t* yrow = reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row) * p.ldy + n0;
+                if (p.wide_out && n0 + 128 <= p.N) {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+                        if (row < p.M) *reinterpret_cast<uint4*>(yrow + 32 * m + 8 * t) = out[m];
+                } else {
+                    // ragged or unaligned rows: through 1 KB of shared memory, 64 columns at a time, written by consecutive lanes
+                    const uint32_t edge = smem_base + P::EDGE_OFFSET + static_cast<uint32_t>(warp - 4) * 1024u;
+                    uint16_t* ytop = reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row0 + 8 * i) * p.ldy + n0;
+                    const int rows = min(8, p.M - row0 - 8 * i);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        __syncwarp();
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(edge + r4 * 128 + m * 64 + t * 16), "r"(out[2 * c + m].x),
+                                         "r"(out[2 * c + m].y), "r"(out[2 * c + m].z), "r"(out[2 * c + m].w)
+                                         : "memory");
+                        __syncwarp();
+                        for (int r = 0; r < rows; ++r)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const int col = c * 64 + 32 * h + lane;
+                                uint16_t e;
+                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(e) : "r"(edge + r * 128 + 64 * h + 2 * lane) : "memory");
+                                if (n0 + col < p.N) ytop[r * p.ldy + col] = e;
+                            }
+                    }
                 }
             }
         }
-        if (lane == 0) bulk_wait_group_all();  // this warp's stores are performed before the CTA leaves
     }
 
     if constexpr (PAIR) {
-        if (warp == 1 && lane == 0 && cta_rank == 0 && *abort_flag != 0) umma_drain<true>(bar_base + 200u);  // let issued MMAs finish first
+        if (warp == 1 && lane == 0 && cta_rank == 0 && *abort_flag != 0) umma_drain<true>(drain_bar);  // let issued MMAs finish first
         tc_fence_before_sync();
         cluster_sync_all();  // neither CTA leaves while the other may still read its operands or signal its barriers
         if (warp == 1) {
@@ -463,7 +573,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             tmem_dealloc_pair(tmem_base, 512);
         }
     } else {
-        if (warp == 1 && lane == 0 && *abort_flag != 0) umma_drain(bar_base + 200u);
+        if (warp == 1 && lane == 0 && *abort_flag != 0) umma_drain(drain_bar);
         tc_fence_before_sync();
         __syncthreads();
         if (warp == 1) {
@@ -474,7 +584,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
 }
 
 template <int BN, bool PAIR, bool QKV>
-dirotq_status_t launch_plan(const MxGemmArgs& a, const CUtensorMap& tmap_y, MxKernelParams& p, cudaStream_t stream) {
+dirotq_status_t launch_plan(const MxGemmArgs& a, const MxKernelParams& p, cudaStream_t stream) {
     using P = MxPlan<BN, PAIR>;
     auto kern = mx_gemm_kernel<BN, PAIR, QKV>;
     const int device = a.b->device, sms = sm_count(device);
@@ -485,9 +595,9 @@ dirotq_status_t launch_plan(const MxGemmArgs& a, const CUtensorMap& tmap_y, MxKe
     cudaError_t err;
     if constexpr (PAIR) {
         const int pairs = static_cast<int>(tiles < sms / 2 ? tiles : sms / 2);
-        err = launch_kernel_pairs(kern, 2 * pairs, NUM_THREADS, P::SMEM_BYTES, stream, true, a.a->tmap, a.b->tmap, tmap_y, p);
+        err = launch_kernel_pairs(kern, 2 * pairs, NUM_THREADS, P::SMEM_BYTES, stream, true, a.a->tmap, a.b->tmap, p);
     } else {
-        err = launch_kernel(kern, static_cast<int>(tiles < sms ? tiles : sms), NUM_THREADS, P::SMEM_BYTES, stream, true, a.a->tmap, a.b->tmap, tmap_y, p);
+        err = launch_kernel(kern, static_cast<int>(tiles < sms ? tiles : sms), NUM_THREADS, P::SMEM_BYTES, stream, true, a.a->tmap, a.b->tmap, p);
     }
     if (err != cudaSuccess) set_error("mx_gemm_kernel", err);
     return err == cudaSuccess ? DIROTQ_OK : DIROTQ_ERR_CUDA;
@@ -510,14 +620,7 @@ dirotq_status_t launch_mx_gemm(const MxGemmArgs& a, cudaStream_t stream) {
     p.status = a.status;
     p.f16 = a.y_dtype == DIROTQ_DTYPE_F16;
     p.early = a.early_weights;
-    p.tma_out = (reinterpret_cast<uintptr_t>(a.y) & 15u) == 0 && a.ldy % 8 == 0;
-    CUtensorMap tmap_y = a.a->tmap;  // (not used without TMA stores)
-    if (p.tma_out) {
-        const dirotq_status_t st =
-            encode_tmap_2d(&tmap_y, p.f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.y, (uint64_t)p.N, (uint64_t)p.M,
-                           (uint64_t)a.ldy * 2, 64, 32, CU_TENSOR_MAP_SWIZZLE_128B);
-        if (st != DIROTQ_OK) return st;
-    }
+    p.wide_out = (reinterpret_cast<uintptr_t>(a.y) & 15u) == 0 && a.ldy % 8 == 0;
     if (a.qk) {
         const dirotq_qk_t& qk = *a.qk;
         p.q_cols = qk.heads_q * qk.head_dim;
@@ -533,12 +636,13 @@ dirotq_status_t launch_mx_gemm(const MxGemmArgs& a, cudaStream_t stream) {
         p.cos_table = qk.cos_table;
         p.sin_table = qk.sin_table;
         p.ld_table = qk.ld_table;
+        p.wide_table = ((reinterpret_cast<uintptr_t>(qk.cos_table) | reinterpret_cast<uintptr_t>(qk.sin_table)) & 15u) == 0 && qk.ld_table % 4 == 0;
         p.num_positions = qk.num_positions;
         p.positions = qk.positions;
     }
     // CTA pairs above 128 rows, where a second row block exists
-    if (p.M > BM) return a.qk ? launch_plan<256, true, true>(a, tmap_y, p, stream) : launch_plan<256, true, false>(a, tmap_y, p, stream);
-    return a.qk ? launch_plan<128, false, true>(a, tmap_y, p, stream) : launch_plan<128, false, false>(a, tmap_y, p, stream);
+    if (p.M > BM) return a.qk ? launch_plan<256, true, true>(a, p, stream) : launch_plan<256, true, false>(a, p, stream);
+    return a.qk ? launch_plan<128, false, true>(a, p, stream) : launch_plan<128, false, false>(a, p, stream);
 }
 
 }  // namespace dirotq
