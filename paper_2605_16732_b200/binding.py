@@ -682,11 +682,12 @@ _DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: 
 
 
 def _row_stride(t: torch.Tensor, width: int) -> int:
-    """Elements between the rows of a 2-D tensor whose rows are contiguous.  A single row's stride says nothing: one that would keep the
+    """Elements between the rows of a 2-D cuda tensor whose rows are contiguous.  A single row's stride says nothing: one that would keep the
     library from wide accesses, or is shorter than the row, is replaced."""
-    assert t.is_cuda and t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1), "rows must be contiguous"
-    if t.shape[0] > 1 or (t.stride(0) >= width and t.stride(0) % 8 == 0):
-        return t.stride(0)
+    s0, s1 = t.stride()
+    assert t.is_cuda and (s1 == 1 or t.shape[1] == 1), "rows of a cuda tensor must be contiguous"
+    if (s0 >= width and s0 % 8 == 0) or t.shape[0] > 1:
+        return s0
     return (max(width, t.shape[1]) + 7) // 8 * 8
 
 
@@ -726,19 +727,22 @@ def dirotq_mxfp4_alloc(rows: int, K: int, device="cuda") -> Mxfp4:
 def dirotq_mxfp4_quantize(x: torch.Tensor, out: Mxfp4 | None = None, scale_rule: int = MX_SCALE_FLOOR, layout: int = LAYOUT_NK,
                           stream=None) -> Mxfp4:
     """x: cuda float32/bfloat16/float16 [rows, K] (LAYOUT_NK) or [K, rows] (LAYOUT_KN), rows of any stride."""
-    rows, K = (x.shape[0], x.shape[1]) if layout == LAYOUT_NK else (x.shape[1], x.shape[0])
+    rows, K = x.shape if layout == LAYOUT_NK else (x.shape[1], x.shape[0])
     if out is None:
         out = dirotq_mxfp4_alloc(rows, K, x.device)
-    assert (out.rows, out.K) == (rows, K), "the operand has another shape"
-    _check(lib().dirotq_mxfp4_quantize(x.data_ptr(), _DTYPES[x.dtype], layout, _row_stride(x, x.shape[1]), scale_rule, out.handle,
-                                       _stream(stream)), "dirotq_mxfp4_quantize")
+    assert out.rows == rows and out.K == K, "the operand has another shape"
+    st = (_lib or lib()).dirotq_mxfp4_quantize(x.data_ptr(), _DTYPES[x.dtype], layout, _row_stride(x, K if layout == LAYOUT_NK else rows), scale_rule,
+                                               out.handle, _stream(stream))
+    if st:
+        _check(st, "dirotq_mxfp4_quantize")
     return out
 
 
 def dirotq_mxfp4_dequantize(t: Mxfp4, y: torch.Tensor, stream=None) -> None:
-    assert tuple(y.shape) == (t.rows, t.K)
-    _check(lib().dirotq_mxfp4_dequantize(t.handle, y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, t.K), _stream(stream)),
-           "dirotq_mxfp4_dequantize")
+    assert y.shape == (t.rows, t.K)
+    st = (_lib or lib()).dirotq_mxfp4_dequantize(t.handle, y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, t.K), _stream(stream))
+    if st:
+        _check(st, "dirotq_mxfp4_dequantize")
 
 
 def dirotq_mxfp4_import(codes: torch.Tensor, scales: torch.Tensor, K: int, out: Mxfp4 | None = None, stream=None) -> Mxfp4:
@@ -767,26 +771,33 @@ def alloc_mxfp4_workspace(M: int, K: int, device="cuda") -> torch.Tensor:
     return _alloc_bytes(out.value, device, zero=True)
 
 
-def _check_bias(bias, y):
-    assert bias is None or (bias.is_cuda and bias.is_contiguous() and bias.dtype == y.dtype and bias.numel() == y.shape[1])
+def _bias_ptr(bias, y, N):
+    if bias is None:
+        return None
+    assert bias.is_cuda and bias.is_contiguous() and bias.dtype == y.dtype and bias.numel() == N
+    return bias.data_ptr()
 
 
 def dirotq_mxfp4_gemm(a: Mxfp4, b: Mxfp4, y: torch.Tensor, workspace: torch.Tensor, bias: torch.Tensor | None = None, stream=None) -> None:
     """y [a.rows, b.rows] (bf16 or f16, rows of any stride) = a b^T + bias."""
-    assert tuple(y.shape) == (a.rows, b.rows)
-    _check_bias(bias, y)
-    _check(lib().dirotq_mxfp4_gemm(a.handle, b.handle, _ptr(bias), y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, b.rows), workspace.data_ptr(),
-                                   workspace.numel(), _stream(stream)), "dirotq_mxfp4_gemm")
+    N = b.rows
+    assert y.shape == (a.rows, N)
+    st = (_lib or lib()).dirotq_mxfp4_gemm(a.handle, b.handle, _bias_ptr(bias, y, N), y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, N),
+                                           workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if st:
+        _check(st, "dirotq_mxfp4_gemm")
 
 
 def dirotq_mxfp4_linear(x: torch.Tensor, w: Mxfp4, y: torch.Tensor, workspace: torch.Tensor, bias: torch.Tensor | None = None,
                         scale_rule: int = MX_SCALE_FLOOR, stream=None) -> None:
     """y [M, w.rows] (bf16 or f16) = x w^T + bias with x [M, K] quantized on the way in."""
-    assert x.shape[1] == w.K and tuple(y.shape) == (x.shape[0], w.rows)
-    _check_bias(bias, y)
-    _check(lib().dirotq_mxfp4_linear(x.data_ptr(), _DTYPES[x.dtype], _row_stride(x, w.K), x.shape[0], scale_rule, w.handle, _ptr(bias), y.data_ptr(),
-                                     _DTYPES[y.dtype], _row_stride(y, w.rows), workspace.data_ptr(), workspace.numel(), _stream(stream)),
-           "dirotq_mxfp4_linear")
+    M, K = x.shape
+    N = w.rows
+    assert K == w.K and y.shape == (M, N)
+    st = (_lib or lib()).dirotq_mxfp4_linear(x.data_ptr(), _DTYPES[x.dtype], _row_stride(x, K), M, scale_rule, w.handle, _bias_ptr(bias, y, N),
+                                             y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, N), workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if st:
+        _check(st, "dirotq_mxfp4_linear")
 
 
 # ------------------------------------------------------------------ queries and keys
@@ -818,27 +829,43 @@ class QkNorm:
             assert cos.is_cuda and sin.is_cuda and cos.dtype == sin.dtype == torch.float32 and cos.shape == sin.shape and cos.shape[1] >= rot // 2
             assert cos.stride() == sin.stride() and (cos.stride(1) == 1 or cos.shape[1] == 1)
             assert positions is None or (positions.is_cuda and positions.is_contiguous() and positions.dtype == torch.int32 and positions.dim() == 1)
-        self.positions = positions
+        self._tokens = None if positions is None else positions.numel()
         self._keep = (q_weight, k_weight, cos, sin, positions)
         self.struct = _QkStruct(heads_q, heads_kv, head_dim, int(norm), float(eps), _DTYPES[weights[0].dtype] if weights else DTYPE_F32, _ptr(q_weight),
                                 _ptr(k_weight), style, rot, _ptr(cos), _ptr(sin), _row_stride(cos, rot // 2) if style else 0, cos.shape[0] if style else 0,
                                 _ptr(positions))
+        self._byref = ctypes.byref(self.struct)
+        self._widths = heads_q * head_dim, heads_kv * head_dim
 
     def _ref(self, M: int):
-        assert self.positions is None or self.positions.numel() == M, "one position per token"
-        return ctypes.byref(self.struct)
+        assert self._tokens is None or self._tokens == M, "one position per token"
+        return self._byref
 
 
 def dirotq_qk_norm_rope(x: torch.Tensor, qk: QkNorm, q_out: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor | None = None,
                         slots: torch.Tensor | None = None, stream=None) -> None:
     """x [M, (heads_q + 2 heads_kv) head_dim]; q_out [M, heads_q head_dim]; k_out, v_out [M or slots, heads_kv head_dim]; slots: cuda int32 [M]."""
-    M, wq, wk = x.shape[0], qk.heads_q * qk.head_dim, qk.heads_kv * qk.head_dim
-    assert x.shape[1] >= wq + (2 if v_out is not None else 1) * wk and q_out.shape[0] == M and q_out.shape[1] >= wq and k_out.shape[1] >= wk
-    assert q_out.dtype == k_out.dtype == x.dtype and (v_out is None or (v_out.dtype == x.dtype and v_out.shape[0] == k_out.shape[0] and v_out.shape[1] >= wk))
-    assert k_out.shape[0] == M if slots is None else (slots.is_cuda and slots.is_contiguous() and slots.dtype == torch.int32 and slots.numel() == M)
-    _check(lib().dirotq_qk_norm_rope(x.data_ptr(), _DTYPES[x.dtype], M, _row_stride(x, wq + 2 * wk), qk._ref(M), q_out.data_ptr(), _row_stride(q_out, wq),
-                                     k_out.data_ptr(), _row_stride(k_out, wk), _ptr(v_out), 0 if v_out is None else _row_stride(v_out, wk), _ptr(slots),
-                                     0 if slots is None else k_out.shape[0], _stream(stream)), "dirotq_qk_norm_rope")
+    wq, wk = qk._widths
+    M, wx = x.shape
+    rows, width = k_out.shape
+    dtype = x.dtype
+    assert q_out.shape[0] == M and q_out.shape[1] >= wq and width >= wk and q_out.dtype == dtype and k_out.dtype == dtype
+    if v_out is None:
+        assert wx >= wq + wk
+        v_ptr, ldv = None, 0
+    else:
+        assert wx >= wq + 2 * wk and v_out.dtype == dtype and v_out.shape[0] == rows and v_out.shape[1] >= wk
+        v_ptr, ldv = v_out.data_ptr(), _row_stride(v_out, wk)
+    if slots is None:
+        assert rows == M
+        s_ptr, rows = None, 0
+    else:
+        assert slots.is_cuda and slots.is_contiguous() and slots.dtype == torch.int32 and slots.numel() == M
+        s_ptr = slots.data_ptr()
+    st = (_lib or lib()).dirotq_qk_norm_rope(x.data_ptr(), _DTYPES[dtype], M, _row_stride(x, wx), qk._ref(M), q_out.data_ptr(), _row_stride(q_out, wq),
+                                             k_out.data_ptr(), _row_stride(k_out, wk), v_ptr, ldv, s_ptr, rows, _stream(stream))
+    if st:
+        _check(st, "dirotq_qk_norm_rope")
 
 
 def dirotq_linear_qkv(x: torch.Tensor, layer: Layer, y: torch.Tensor, workspace: torch.Tensor, qk: QkNorm, stream=None) -> None:
@@ -850,8 +877,10 @@ def dirotq_linear_qkv(x: torch.Tensor, layer: Layer, y: torch.Tensor, workspace:
 def dirotq_mxfp4_qkv(x: torch.Tensor, w: Mxfp4, y: torch.Tensor, workspace: torch.Tensor, qk: QkNorm, bias: torch.Tensor | None = None,
                      scale_rule: int = MX_SCALE_FLOOR, stream=None) -> None:
     """dirotq_mxfp4_linear on a fused q/k/v weight with norm and rotation of q and k before the result is rounded."""
-    assert x.shape[1] == w.K and tuple(y.shape) == (x.shape[0], w.rows)
-    _check_bias(bias, y)
-    _check(lib().dirotq_mxfp4_qkv(x.data_ptr(), _DTYPES[x.dtype], _row_stride(x, w.K), x.shape[0], scale_rule, w.handle, _ptr(bias), qk._ref(x.shape[0]),
-                                  y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, w.rows), workspace.data_ptr(), workspace.numel(), _stream(stream)),
-           "dirotq_mxfp4_qkv")
+    M, K = x.shape
+    N = w.rows
+    assert K == w.K and y.shape == (M, N)
+    st = (_lib or lib()).dirotq_mxfp4_qkv(x.data_ptr(), _DTYPES[x.dtype], _row_stride(x, K), M, scale_rule, w.handle, _bias_ptr(bias, y, N), qk._ref(M),
+                                          y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, N), workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if st:
+        _check(st, "dirotq_mxfp4_qkv")

@@ -661,6 +661,7 @@ dirotq_status_t dirotq_set_gemm_tile(int columns) {
     const bool int4_only = w4a4_plan_exists(columns) && columns != 128 && columns != 256;  // (the other kernels then choose for themselves)
     dirotq_status_t st = set_w4a4_tile_columns(columns);
     if (st == DIROTQ_OK) st = set_nvfp4_tile_columns(int4_only ? 0 : columns);
+    if (st == DIROTQ_OK) st = set_mx_tile_columns(columns == 64 || columns == 128 || columns == 512 ? columns : 0);
     return st != DIROTQ_OK ? st : set_w4a8_tile_columns(int4_only ? 0 : columns);
 }
 

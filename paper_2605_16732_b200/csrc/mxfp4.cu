@@ -3,6 +3,8 @@
 #include "ptx.cuh"
 
 #include <new>
+#include <type_traits>
+
 #include <string.h>
 
 namespace dirotq {
@@ -15,100 +17,109 @@ constexpr int kThreads = 256;
 // 32, so the maximum is two shuffles, a block's codes are four words side by side, a warp's codes 128 bytes.
 constexpr int kUnits = 4;  // units per warp, their loads in flight together
 
-template <typename T, bool WIDE>
-__device__ __forceinline__ void load_row8(const T* row, int k0, int K, float (&v)[8]) {
-    if (WIDE && k0 + 8 <= K) {
-        load8<T>(row + k0, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k0 + i < K ? to_f32<T>(row[k0 + i]) : 0.f;
-    }
-}
-
-template <int RULE>
-__device__ __forceinline__ uint32_t quantize8(const float (&v)[8], uint32_t byte) {
-    const float inv = mx_inverse(byte);
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) w |= to_e2m1x2(v[i] * inv, v[i + 1] * inv) << (4 * i);
-    return byte == 255u ? 0u : w;
-}
-
 template <typename T, int RULE, bool WIDE>
 __global__ void __launch_bounds__(kThreads) mx_quantize_rows_kernel(const T* __restrict__ x, long long ldx, int rows, int K, int nkb, int pitch,
                                                                     uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
     const int lane = threadIdx.x & 31;
-    const long long units = static_cast<long long>(rows) * nkb;
-    const long long first = (static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
+    const unsigned units = static_cast<unsigned>(rows) * nkb;  // (at most 2^31 - 1, see check_shape)
+    const unsigned first = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
+    if (first >= units) return;
+    int row = static_cast<int>(first / nkb), kb = static_cast<int>(first % nkb);
     // the previous kernel of the stream may still read the workspace this one writes, or write x
     grid_dependency_wait();
     grid_launch_dependents();
-    float v[kUnits][8];
+    Raw8<T> raw[kUnits];
+    {
+        int r = row, b = kb;
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-        const long long unit = first + u;
-        if (unit < units) {
-            const int row = static_cast<int>(unit / nkb), kb = static_cast<int>(unit % nkb);
-            load_row8<T, WIDE>(x + row * ldx, kb * 256 + lane * 8, K, v[u]);
+        for (int u = 0; u < kUnits; ++u) {
+            if (r < rows) raw[u] = load_raw8<T>(x + r * ldx, b * 256 + lane * 8, K, WIDE);
+            if (++b == nkb) { b = 0; ++r; }
         }
     }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-        const long long unit = first + u;
-        if (unit >= units) break;  // (the same for the whole warp)
-        const int row = static_cast<int>(unit / nkb), kb = static_cast<int>(unit % nkb);
+        if (row >= rows) break;  // (the same for the whole warp)
+        float v[8];
+        unpack8<T>(raw[u], v);
         uint32_t am = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) am = max(am, __float_as_uint(v[u][i]) & 0x7fffffffu);
+        for (int i = 0; i < 8; ++i) am = max(am, __float_as_uint(v[i]) & 0x7fffffffu);
         am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
         am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
         const int k0 = kb * 256 + lane * 8;
         const uint32_t byte = mx_scale_byte<RULE>(am);
-        const uint32_t word = quantize8<RULE>(v[u], byte);
+        const uint32_t word = mx_codes8(v, byte);
         if (k0 < pitch * 2) *reinterpret_cast<uint32_t*>(codes + static_cast<size_t>(row) * pitch + k0 / 2) = word;
         // lane 16 h gathers the bytes of blocks 4 h .. 4 h + 3 of the unit
         uint32_t sw = byte << (8 * ((lane >> 2) & 3));
         sw |= __shfl_xor_sync(0xffffffffu, sw, 4);
         sw |= __shfl_xor_sync(0xffffffffu, sw, 8);
         if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(scales + mx_scale_word(row, kb * 2 + (lane >> 4), nkb)) = sw;
+        if (++kb == nkb) { kb = 0; ++row; }
     }
 }
 
 // ------------------------------------------------------------------ quantizer, elements along a column (weights stored [K, N])
-// A block of threads takes 32 columns x 256 elements along K: a thread has one column's block of 32 in registers (the lanes of a warp read
-// consecutive columns), codes leave through shared memory so that a column's 128 bytes are written together.
-template <typename T, int RULE>
+// A block of threads takes COLS * 32 columns x 256 elements along K: a thread has a block of 32 of one column (COLS = 1), or of two adjacent ones
+// in 16 bits (COLS = 2: pairs of values are loaded as words, so that a warp reads whole 128-byte lines either way).  Codes leave through
+// shared memory so that a column's 128 bytes are written together.
+template <typename T, int RULE, int COLS>
 __global__ void __launch_bounds__(kThreads) mx_quantize_cols_kernel(const T* __restrict__ x, long long ldx, int rows, int K, int nkb, int pitch,
                                                                     uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-    __shared__ uint4 s_codes[32][9];  // (a row of padding: the threads of a warp write different columns' rows)
-    __shared__ __align__(16) uint8_t s_scales[32][8];
+    constexpr int WIDTH = 32 * COLS;
+    __shared__ uint4 s_codes[WIDTH][9];  // (a piece of padding: the threads of a warp write different columns' rows)
+    __shared__ __align__(16) uint8_t s_scales[WIDTH][8];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int kb = blockIdx.x % nkb;
-    const int row0 = blockIdx.x / nkb * 32;
-    const int row = row0 + lane, k0 = kb * 256 + w * 32;
+    const int row0 = blockIdx.x / nkb * WIDTH;
+    const int row = row0 + lane * COLS, k0 = kb * 256 + w * 32;
     grid_dependency_wait();
     grid_launch_dependents();
-    float v[32];
-    uint32_t am = 0;
+    using Word = std::conditional_t<COLS == 2, uint32_t, T>;
+    Word raw[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = row < rows && k0 + i < K ? to_f32<T>(x[(k0 + i) * ldx + row]) : 0.f;
+    for (int i = 0; i < 32; ++i) {
+        raw[i] = Word();
+        if (row < rows && k0 + i < K) raw[i] = *reinterpret_cast<const Word*>(x + (k0 + i) * ldx + row);
+    }
 #pragma unroll
-    for (int i = 0; i < 32; ++i) am = max(am, __float_as_uint(v[i]) & 0x7fffffffu);
-    const uint32_t byte = mx_scale_byte<RULE>(am);
-    const float inv = mx_inverse(byte);
-    uint32_t c[4] = {0, 0, 0, 0};
+    for (int c = 0; c < COLS; ++c) {
+        auto value = [&](int i) {
+            if constexpr (COLS == 2) {
+                union { uint32_t u; T t[2]; } both;
+                both.u = raw[i];
+                return to_f32<T>(both.t[c]);
+            } else {
+                return to_f32<T>(raw[i]);
+            }
+        };
+        uint32_t am = 0;
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) c[i >> 3] |= to_e2m1x2(v[i] * inv, v[i + 1] * inv) << (4 * (i & 7));
-    s_codes[lane][w] = byte == 255u ? make_uint4(0, 0, 0, 0) : make_uint4(c[0], c[1], c[2], c[3]);
-    s_scales[lane][w] = static_cast<uint8_t>(byte);
+        for (int i = 0; i < 32; ++i) am = max(am, __float_as_uint(value(i)) & 0x7fffffffu);
+        const uint32_t byte = mx_scale_byte<RULE>(am);
+        uint32_t words[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = value(8 * g + i);
+            words[g] = mx_codes8(v, byte);
+        }
+        s_codes[lane * COLS + c][w] = make_uint4(words[0], words[1], words[2], words[3]);
+        s_scales[lane * COLS + c][w] = static_cast<uint8_t>(byte);
+    }
     __syncthreads();
-    const int r = threadIdx.x >> 3, piece = threadIdx.x & 7;  // 32 columns x 8 pieces of 16 bytes
-    if (row0 + r < rows) {
-        const int at = kb * 128 + piece * 16;
-        if (at < pitch) *reinterpret_cast<uint4*>(codes + static_cast<size_t>(row0 + r) * pitch + at) = s_codes[r][piece];
-        if (piece < 2)
-            *reinterpret_cast<uint32_t*>(scales + mx_scale_word(row0 + r, kb * 2 + piece, nkb)) =
-                *reinterpret_cast<const uint32_t*>(&s_scales[r][piece * 4]);
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) {
+        const int r = i * 32 + (threadIdx.x >> 3), piece = threadIdx.x & 7;  // columns x 8 pieces of 16 bytes
+        if (row0 + r < rows) {
+            const int at = kb * 128 + piece * 16;
+            if (at < pitch) *reinterpret_cast<uint4*>(codes + static_cast<size_t>(row0 + r) * pitch + at) = s_codes[r][piece];
+            if (piece < 2)
+                *reinterpret_cast<uint32_t*>(scales + mx_scale_word(row0 + r, kb * 2 + piece, nkb)) =
+                    *reinterpret_cast<const uint32_t*>(&s_scales[r][piece * 4]);
+        }
     }
 }
 
@@ -117,25 +128,29 @@ template <typename T, bool WIDE>
 __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int K,
                                                                  int nkb, int pitch, T* __restrict__ y, long long ldy) {
     const int lane = threadIdx.x & 31;
-    const long long units = static_cast<long long>(rows) * nkb;
-    const long long first = (static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
+    const unsigned units = static_cast<unsigned>(rows) * nkb;
+    const unsigned first = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
+    if (first >= units) return;
+    int row = static_cast<int>(first / nkb), kb = static_cast<int>(first % nkb);
     grid_dependency_wait();
     grid_launch_dependents();
     uint32_t word[kUnits], sw[kUnits];
+    {
+        int r = row, b = kb;
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-        const long long unit = first + u;
-        if (unit >= units) continue;
-        const int row = static_cast<int>(unit / nkb), kb = static_cast<int>(unit % nkb);
-        const int k0 = kb * 256 + lane * 8;
-        word[u] = k0 < pitch * 2 ? *reinterpret_cast<const uint32_t*>(codes + static_cast<size_t>(row) * pitch + k0 / 2) : 0u;
-        sw[u] = *reinterpret_cast<const uint32_t*>(scales + mx_scale_word(row, kb * 2 + (lane >> 4), nkb));
+        for (int u = 0; u < kUnits; ++u) {
+            word[u] = sw[u] = 0;
+            if (r < rows) {
+                const int k0 = b * 256 + lane * 8;
+                if (k0 < pitch * 2) word[u] = *reinterpret_cast<const uint32_t*>(codes + static_cast<size_t>(r) * pitch + k0 / 2);
+                sw[u] = *reinterpret_cast<const uint32_t*>(scales + mx_scale_word(r, b * 2 + (lane >> 4), nkb));
+            }
+            if (++b == nkb) { b = 0; ++r; }
+        }
     }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-        const long long unit = first + u;
-        if (unit >= units) break;
-        const int row = static_cast<int>(unit / nkb), kb = static_cast<int>(unit % nkb);
+        if (row >= rows) break;
         const int k0 = kb * 256 + lane * 8;
         const float s = e8m0_value((sw[u] >> (8 * ((lane >> 2) & 3))) & 0xffu);
         float v[8];
@@ -147,12 +162,15 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* 
         }
         T* out = y + row * ldy;
         if (WIDE && k0 + 8 <= K) {
-            store8<T>(out + k0, v);
+            const Raw8<T> r = pack8<T>(v);
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) reinterpret_cast<uint4*>(out + k0)[i] = r.u[i];
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (k0 + i < K) out[k0 + i] = from_f32<T>(v[i]);
         }
+        if (++kb == nkb) { kb = 0; ++row; }
     }
 }
 
@@ -212,11 +230,20 @@ cudaError_t quantize_t(const void* x, int layout, long long ldx, int rule, const
     uint8_t* scales = codes + t->lay.off_scales;
     const bool floor = rule == DIROTQ_MX_SCALE_FLOOR;
     const bool wide = wide_rows(x, ldx, sizeof(T) == 4 ? DIROTQ_DTYPE_F32 : DIROTQ_DTYPE_BF16);
-    auto kern = layout == DIROTQ_LAYOUT_KN
-                    ? (floor ? mx_quantize_cols_kernel<T, DIROTQ_MX_SCALE_FLOOR> : mx_quantize_cols_kernel<T, DIROTQ_MX_SCALE_CEIL>)
-                : wide ? (floor ? mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_FLOOR, true> : mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_CEIL, true>)
-                       : (floor ? mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_FLOOR, false> : mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_CEIL, false>);
-    const unsigned blocks = layout == DIROTQ_LAYOUT_KN ? static_cast<unsigned>((t->rows + 31) / 32) * t->lay.nkb : unit_blocks(t->rows, t->lay.nkb);
+    auto rows_kern = wide ? (floor ? mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_FLOOR, true> : mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_CEIL, true>)
+                          : (floor ? mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_FLOOR, false> : mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_CEIL, false>);
+    if (layout == DIROTQ_LAYOUT_NK)
+        return launch_kernel(rows_kern, static_cast<int>(unit_blocks(t->rows, t->lay.nkb)), kThreads, 0, stream, true, in, ldx, t->rows, t->K, t->lay.nkb,
+                             t->lay.pitch, codes, scales);
+    auto kern = floor ? mx_quantize_cols_kernel<T, DIROTQ_MX_SCALE_FLOOR, 1> : mx_quantize_cols_kernel<T, DIROTQ_MX_SCALE_CEIL, 1>;
+    int width = 32;
+    if constexpr (sizeof(T) == 2) {
+        if (t->rows % 2 == 0 && ldx % 2 == 0 && (reinterpret_cast<uintptr_t>(x) & 3u) == 0) {  // pairs of columns are aligned words
+            kern = floor ? mx_quantize_cols_kernel<T, DIROTQ_MX_SCALE_FLOOR, 2> : mx_quantize_cols_kernel<T, DIROTQ_MX_SCALE_CEIL, 2>;
+            width = 64;
+        }
+    }
+    const unsigned blocks = static_cast<unsigned>((t->rows + width - 1) / width) * t->lay.nkb;
     return launch_kernel(kern, static_cast<int>(blocks), kThreads, 0, stream, true, in, ldx, t->rows, t->K, t->lay.nkb, t->lay.pitch, codes, scales);
 }
 
@@ -279,12 +306,16 @@ dirotq_status_t linear(const void* x, int x_dtype, long long ldx, int M, int sca
     }
     st = check_operand(w);
     if (st != DIROTQ_OK) return st;
+    if (mx_fuses(M, w->rows, w->lay.nkb, qk, w->device)) {
+        const MxGemmArgs ga = {M, nullptr, x, x_dtype, ldx, scale_rule, w, bias, y, y_dtype, ldy, static_cast<int*>(workspace), false, qk};
+        return launch_mx_gemm(ga, stream);
+    }
     dirotq_mxfp4 a;
-    st = mx_setup(&a, M, w->K, static_cast<char*>(workspace) + kAlign, w->device);
+    st = mx_setup(&a, M, w->K, static_cast<char*>(workspace) + kAlign, w->device, false);
     if (st != DIROTQ_OK) return st;
     st = done("dirotq_mxfp4_linear", launch_mx_quantize(x, x_dtype, DIROTQ_LAYOUT_NK, ldx, scale_rule, &a, stream));
     if (st != DIROTQ_OK) return st;
-    const MxGemmArgs ga = {&a, w, bias, y, y_dtype, ldy, static_cast<int*>(workspace), true, qk};
+    const MxGemmArgs ga = {M, &a, nullptr, 0, 0, 0, w, bias, y, y_dtype, ldy, static_cast<int*>(workspace), true, qk};
     return launch_mx_gemm(ga, stream);
 }
 
@@ -292,7 +323,7 @@ dirotq_status_t linear(const void* x, int x_dtype, long long ldx, int M, int sca
 
 bool mx_valid(const dirotq_mxfp4* t) { return t != nullptr && t->magic == kMxMagic; }
 
-dirotq_status_t mx_setup(dirotq_mxfp4* t, int rows, int K, void* buffer, int device) {
+dirotq_status_t mx_setup(dirotq_mxfp4* t, int rows, int K, void* buffer, int device, bool both) {
     memset(t, 0, sizeof *t);
     t->magic = kMxMagic;
     t->device = device;
@@ -301,6 +332,12 @@ dirotq_status_t mx_setup(dirotq_mxfp4* t, int rows, int K, void* buffer, int dev
     t->lay = make_mx_layout(rows, K);
     t->buffer = static_cast<char*>(buffer);
     t->box = box_rows(rows);
+    t->box64 = rows < 64 ? t->box : 64;
+    if (both) {
+        const dirotq_status_t st = encode_tmap_2d(&t->tmap64, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, buffer, (uint64_t)t->lay.pitch, (uint64_t)rows,
+                                                  (uint64_t)t->lay.pitch, 128, t->box64, CU_TENSOR_MAP_SWIZZLE_128B);
+        if (st != DIROTQ_OK) return st;
+    }
     return encode_tmap_2d(&t->tmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, buffer, (uint64_t)t->lay.pitch, (uint64_t)rows, (uint64_t)t->lay.pitch, 128,
                           t->box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
@@ -337,7 +374,7 @@ dirotq_status_t dirotq_mxfp4_create(int rows, int K, void* buffer, size_t buffer
     if (st != DIROTQ_OK) return st;
     dirotq_mxfp4* t = new (std::nothrow) dirotq_mxfp4;
     if (!t) return DIROTQ_ERR_INVALID_ARG;
-    st = mx_setup(t, rows, K, buffer, dev);
+    st = mx_setup(t, rows, K, buffer, dev, true);
     if (st != DIROTQ_OK) {
         delete t;
         return st;
@@ -432,7 +469,7 @@ dirotq_status_t dirotq_mxfp4_gemm(const dirotq_mxfp4_t* a, const dirotq_mxfp4_t*
     st = check_operand(a);
     if (st == DIROTQ_OK) st = check_operand(b);
     if (st != DIROTQ_OK) return st;
-    const MxGemmArgs ga = {a, b, bias, y, y_dtype, ldy, static_cast<int*>(workspace), false, nullptr};
+    const MxGemmArgs ga = {a->rows, a, nullptr, 0, 0, 0, b, bias, y, y_dtype, ldy, static_cast<int*>(workspace), false, nullptr};
     return launch_mx_gemm(ga, static_cast<cudaStream_t>(stream));
 }
 

@@ -43,6 +43,8 @@ struct dirotq_mxfp4 {
     char* buffer;      // device
     int box;           // rows of the tensor map's box: 128, or the rows that exist rounded up to 8 (box_rows)
     CUtensorMap tmap;  // u8 [rows][pitch], box 128 x box, 128B swizzle
+    int box64;           // the same with boxes of up to 64 rows (tiles of 64 columns)
+    CUtensorMap tmap64;
 };
 
 namespace dirotq {
@@ -50,7 +52,7 @@ namespace dirotq {
 constexpr uint32_t kMxMagic = 0x4678694du;  // "Mixf"
 
 // Host side of the operand (mxfp4.cu); `t` need not come from dirotq_mxfp4_create.
-dirotq_status_t mx_setup(dirotq_mxfp4* t, int rows, int K, void* buffer, int device);
+dirotq_status_t mx_setup(dirotq_mxfp4* t, int rows, int K, void* buffer, int device, bool both);  // both: the map with boxes of 64 rows too
 bool mx_valid(const dirotq_mxfp4* t);
 inline size_t dtype_size(int dtype) { return dtype == DIROTQ_DTYPE_F32 ? 4 : 2; }
 inline bool dtype_is_16(int dtype) { return dtype == DIROTQ_DTYPE_BF16 || dtype == DIROTQ_DTYPE_F16; }
@@ -60,7 +62,12 @@ inline bool dtype_ok(int dtype) { return dtype == DIROTQ_DTYPE_F32 || dtype_is_1
 cudaError_t launch_mx_quantize(const void* x, int x_dtype, int x_layout, long long ldx, int scale_rule, const dirotq_mxfp4* t,
                                cudaStream_t stream);
 struct MxGemmArgs {
-    const dirotq_mxfp4* a;
+    int M;
+    const dirotq_mxfp4* a;   // NULL: the kernel quantizes x itself (mx_fuses)
+    const void* x;
+    int x_dtype;
+    long long ldx;
+    int scale_rule;
     const dirotq_mxfp4* b;
     const void* bias;
     void* y;
@@ -71,6 +78,7 @@ struct MxGemmArgs {
     const dirotq_qk_t* qk;   // norm and rotation in the epilogue, or NULL
 };
 dirotq_status_t launch_mx_gemm(const MxGemmArgs& a, cudaStream_t stream);
+bool mx_fuses(int M, int N, int nkb, const dirotq_qk_t* qk, int device);  // whether dirotq_mxfp4_linear / _qkv leaves x to the product's kernel
 
 // qk_norm.cu
 dirotq_status_t qk_check(const dirotq_qk_t* qk, int M);
@@ -95,8 +103,8 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t abits) {
     if (RULE == DIROTQ_MX_SCALE_CEIL) b += (abits & 0x7fffffu) > 0x400000u ? 1 : 0;
     return static_cast<uint32_t>(b < 0 ? 0 : b);
 }
-// What elements are multiplied by: 2^(127 - byte), exact (byte 0: 2^127; the largest byte of a number is 253).  0 for a NaN block,
-// whose infinities and NaN are then replaced (mx_clean).
+// What elements are multiplied by: 2^(127 - byte), exact (byte 0: 2^127; the largest byte of a number is 253).  (A NaN
+// block's codes are cleared.)
 __device__ __forceinline__ float mx_inverse(uint32_t byte) { return byte == 255u ? 0.f : pow2f(127 - static_cast<int>(byte)); }
 
 __device__ __forceinline__ uint32_t to_e2m1x2(float lo, float hi) {  // nearest, ties to even, saturating; `lo` in bits 0..3
@@ -123,6 +131,15 @@ __device__ __forceinline__ float2 from_e2m1x2(uint32_t byte) {
     return __half22float2(*reinterpret_cast<const __half2*>(&h2));
 }
 
+// The codes of eight elements of a block with this scale byte, the first in bits 0..3.
+__device__ __forceinline__ uint32_t mx_codes8(const float (&v)[8], uint32_t byte) {
+    const float inv = mx_inverse(byte);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) w |= to_e2m1x2(v[i] * inv, v[i + 1] * inv) << (4 * i);
+    return byte == 255u ? 0u : w;
+}
+
 template <typename T>
 __device__ __forceinline__ float to_f32(T v);
 template <>
@@ -140,30 +157,40 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { retu
 template <>
 __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
-// Eight elements, 16-byte aligned, to and from fp32.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
-    if constexpr (sizeof(T) == 4) {
-        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-        union { uint4 u; T t[8]; } c;
-        c.u = *reinterpret_cast<const uint4*>(p);
+struct Raw8 {  // eight elements as they lie in memory
+    uint4 u[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&v)[8]) {
+    union { Raw8<T> r; T t[8]; } c;
+    c.r = r;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_f32<T>(c.t[i]);
-    }
+    for (int i = 0; i < 8; ++i) v[i] = to_f32<T>(c.t[i]);
 }
+// Elements k0 .. k0 + 7 of a row of K as they are, zeros behind K.  (Not converted here: a conversion would wait for the load, and several are to be
+// in flight.)
 template <typename T>
-__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
-    if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-        union { uint4 u; T t[8]; } c;
+__device__ __forceinline__ Raw8<T> load_raw8(const T* row, int k0, int K, bool wide) {
+    Raw8<T> r;
+    if (wide && k0 + 8 <= K) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c.t[i] = from_f32<T>(v[i]);
-        *reinterpret_cast<uint4*>(p) = c.u;
+        for (int u = 0; u < static_cast<int>(sizeof(T) / 2); ++u) r.u[u] = reinterpret_cast<const uint4*>(row + k0)[u];
+    } else {
+        union { Raw8<T> r; T t[8]; } c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c.t[i] = k0 + i < K ? row[k0 + i] : from_f32<T>(0.f);
+        r = c.r;
     }
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ Raw8<T> pack8(const float (&v)[8]) {
+    union { Raw8<T> r; T t[8]; } c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c.t[i] = from_f32<T>(v[i]);
+    return c.r;
 }
 
 }  // namespace dirotq

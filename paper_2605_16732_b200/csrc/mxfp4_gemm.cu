@@ -10,15 +10,20 @@
 // to the MMA warp through an mbarrier.  An atom's 32-bit words hold the scales of two instructions; the instruction descriptor's scale
 // ids (0 or 2) pick the half.
 //
-// Roles (384 threads): warp 0 TMA producer, warp 1 MMA issuer and owner of the tensor memory, warps 2..3 scale copiers, warps 4..11 epilogue,
-// a warpgroup per 128 columns.  Plans:
+// Roles (384 threads): warp 0 TMA producer, warp 1 MMA issuer and owner of the tensor memory, warps 2..3 scale copiers, warps 4..11 epilogue in
+// two warpgroups.  Plans:
 //   PAIR: clusters of two CTAs share every MMA (cta_group::2, M = 256): 256 rows x 256 columns per pair; each CTA holds its own 128 rows of
-//         a, half of b's 256 rows, and the scales of both halves.  One 256-column accumulator: the epilogue reads it into registers and
-//         hands it back before it converts.
-//   single CTAs, 128 x 128: two accumulators, the two epilogue warpgroups take tiles in turn.
+//         a, half of b's 256 rows, and the scales of both halves.  One 256-column accumulator, a warpgroup per half of it: the epilogue
+//         reads it into registers and hands it back before it converts.
+//   single CTAs, 128 rows x 128 or 64 columns: two accumulators, the two epilogue warpgroups take tiles in turn.
+//   FUSE (single CTAs, few rows): the activations are quantized by the kernel itself, by every CTA for itself, into shared memory, where
+//         their codes and scales stay; the ring carries b alone.
 // Every plan adds an output element's products in the same order, so that a row's bits do not depend on the plan.
 #include "mxfp4.cuh"
 #include "ptx.cuh"
+
+#include <atomic>
+#include <type_traits>
 
 namespace dirotq {
 namespace {
@@ -29,25 +34,31 @@ constexpr int A_BYTES = BM * 128;      // 16 KB
 constexpr int NUM_THREADS = 384;
 constexpr int NUM_EPI_WARPS = 8;
 
-template <int BN, bool PAIR>
+template <int BN, bool PAIR, bool FUSE>
 struct MxPlan {
-    static constexpr int NB = BN / 128;             // 128-column blocks of a tile
-    static constexpr int B_BYTES = 128 * 128;       // this CTA's rows of b: the tile's (single) or half of them (pair)
-    static constexpr int STAGE_BYTES = A_BYTES + B_BYTES + (1 + NB) * ATOMS;  // 34 / 35 KB
-    static constexpr int STAGES = 6;
-    static constexpr int ACC_BUFS = PAIR ? 1 : 2;
-    static constexpr int BAR_OFFSET = STAGES * STAGE_BYTES;
-    static constexpr int BIAS_OFFSET = BAR_OFFSET + 256;                         // per warpgroup two buffers of 128 values
-    static constexpr int HEADW_OFFSET = BIAS_OFFSET + 4 * 128 * 4;               // q and k weights of a head, 128 values each
-    static constexpr int EDGE_OFFSET = HEADW_OFFSET + 2 * 128 * 4;               // 8 rows x 128 bytes per epilogue warp: rows of y of any alignment
+    static constexpr int NB = BN == 256 ? 2 : 1;                              // 128-column blocks whose scales a stage holds
+    static constexpr int A_STAGE = FUSE ? 0 : A_BYTES;
+    static constexpr int B_BYTES = (PAIR ? BN / 2 : BN) * 128;                // this CTA's rows of b: the tile's (single) or half of them (pair)
+    static constexpr int SF_OFFSET = A_STAGE + B_BYTES;                       // scales of a (unless they stay), then of b
+    static constexpr int SFB_OFFSET = SF_OFFSET + (FUSE ? 0 : ATOMS);
+    static constexpr int STAGE_BYTES = SFB_OFFSET + NB * ATOMS;               // pair 35 KB, single 34 / 26 KB, fused 17 / 9 KB
+    static constexpr int STAGES = FUSE ? (BN == 64 ? 10 : 6) : (BN == 64 ? 8 : 6);
+    static constexpr int RESIDENT = FUSE ? (BN == 64 ? 120 : 112) * 1024 : 0; // codes and scales of the activations
+    static constexpr int BAR_OFFSET = RESIDENT + STAGES * STAGE_BYTES;
+    static constexpr int BIAS_OFFSET = BAR_OFFSET + 512;                      // per warpgroup two buffers of 128 values
+    static constexpr int HEADW_OFFSET = BIAS_OFFSET + 4 * 128 * 4;            // q and k weights of a head, 128 values each
+    static constexpr int EDGE_OFFSET = HEADW_OFFSET + 2 * 128 * 4;            // 8 rows x 128 bytes per epilogue warp: rows of y of any alignment
     static constexpr int SMEM_BYTES = EDGE_OFFSET + NUM_EPI_WARPS * 1024 + 1024;
-    static constexpr int TMEM_SF = ACC_BUFS * BN;   // columns of the scales: per stage 8 for a, 8 per 128 columns
+    static constexpr int ACC_BUFS = PAIR ? 1 : 2;
+    static constexpr int TMEM_SF = ACC_BUFS * BN;                             // columns of the scales: per stage 8 for a, 8 per 128 columns
     static constexpr int SF_COLS = 8 * (1 + NB);
-    static_assert(PAIR ? BN == 256 : BN == 128, "plans");
+    static_assert(PAIR ? BN == 256 && !FUSE : BN == 128 || BN == 64, "plans");
     static_assert(TMEM_SF + STAGES * SF_COLS <= 512, "tensor memory plan");
-    static_assert(8 * ((PAIR ? 4 : 3) * STAGES + 4) <= 240, "barriers end below the words at +240");
+    static_assert(8 * ((PAIR ? 4 : 3) * STAGES + 5) <= 480, "barriers end below the words at +480");
     static_assert(SMEM_BYTES <= 232448, "shared memory plan");
     static_assert(STAGE_BYTES % 1024 == 0, "operand tiles must stay 1024-byte aligned");
+    // (an MMA reads 128 rows wherever fewer are kept: past the last ones it reads what lies behind, whose results are not stored)
+    static_assert(!FUSE || STAGES * STAGE_BYTES >= A_BYTES, "a k-block's 128 rows end inside the ring");
 };
 
 struct MxKernelParams {
@@ -59,7 +70,6 @@ struct MxKernelParams {
     uint8_t* y;
     long long ldy;
     int* status;
-    int f16;               // y and bias are fp16 (else bf16)
     int wide_out;          // rows of y are 16-byte aligned
     int early;             // b may be read while the previous kernel runs
     // norm and rotation of q and k
@@ -76,6 +86,12 @@ struct MxKernelParams {
     int wide_table;        // rows of both tables are 16-byte aligned
     int num_positions;
     const int32_t* positions;
+    // FUSE: the activations as they are
+    const void* x;
+    long long ldx;
+    int x_dtype, x_wide;   // x_wide: rows are 16-byte aligned
+    int K, scale_rule;
+    int groups;            // blocks of 8 rows that exist
 };
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -132,8 +148,9 @@ __device__ __forceinline__ float load_16(const void* p, int i, int f16) {
 __device__ __forceinline__ float load_weight(const void* p, int i, int dtype) {
     return p == nullptr ? 1.f : dtype == DIROTQ_DTYPE_F32 ? __ldg(static_cast<const float*>(p) + i) : load_16(p, i, dtype == DIROTQ_DTYPE_F16);
 }
-__device__ __forceinline__ uint32_t pack2(float lo, float hi, int f16) {
-    if (f16) {
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    if constexpr (F16) {
         const __half2 v = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&v);
     }
@@ -266,25 +283,81 @@ __device__ __forceinline__ void head_norm_rope(float (*v)[8], bool turned, const
     }
 }
 
-template <int BN, bool PAIR, bool QKV>
+// Quantizes all M rows into shared memory (256 threads): codes at `codes` + (kb groups + row / 8) KB in the layout of a TMA load with the 128-byte
+// swizzle, scales at `scales` + kb KB as two atoms.  The arithmetic of mx_quantize_rows_kernel.
+template <typename T>
+__device__ __forceinline__ void quantize_resident(const MxKernelParams& p, uint32_t codes, uint32_t scales, int warp, int lane) {
+    constexpr int AHEAD = 2;  // a warp's units (256 elements of a row), computed side by side
+    const T* x = static_cast<const T*>(p.x);
+    const int units = p.M * p.nkb;
+    int row = warp / p.nkb, kb = warp - row * p.nkb;
+    const int rows_on = NUM_EPI_WARPS / p.nkb, kb_on = NUM_EPI_WARPS - rows_on * p.nkb;
+#pragma unroll 1
+    for (int u0 = warp; u0 < units; u0 += AHEAD * NUM_EPI_WARPS) {
+        Raw8<T> raw[AHEAD];
+        int rows[AHEAD], kbs[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            rows[j] = row;
+            kbs[j] = kb;
+            raw[j] = Raw8<T>();
+            if (row < p.M) raw[j] = load_raw8<T>(x + row * p.ldx, kb * 256 + lane * 8, p.K, p.x_wide != 0);
+            row += rows_on;
+            kb += kb_on;
+            if (kb >= p.nkb) {
+                kb -= p.nkb;
+                ++row;
+            }
+        }
+        uint32_t word[AHEAD], sw[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            float v[8];
+            unpack8<T>(raw[j], v);
+            uint32_t am = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) am = max(am, __float_as_uint(v[i]) & 0x7fffffffu);
+            am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
+            am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
+            const uint32_t byte = p.scale_rule == DIROTQ_MX_SCALE_FLOOR ? mx_scale_byte<DIROTQ_MX_SCALE_FLOOR>(am) : mx_scale_byte<DIROTQ_MX_SCALE_CEIL>(am);
+            word[j] = mx_codes8(v, byte);
+            sw[j] = byte << (8 * ((lane >> 2) & 3));
+            sw[j] |= __shfl_xor_sync(0xffffffffu, sw[j], 4);
+            sw[j] |= __shfl_xor_sync(0xffffffffu, sw[j], 8);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (rows[j] >= p.M) break;
+            const uint32_t dst = codes + (kbs[j] * p.groups + (rows[j] >> 3)) * 1024 + (rows[j] & 7) * 128 + (((lane >> 2) ^ (rows[j] & 7)) << 4) + (lane & 3) * 4;
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst), "r"(word[j]) : "memory");
+            if ((lane & 15) == 0)
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(scales + kbs[j] * ATOMS + (lane >> 4) * 512 + (rows[j] & 31) * 16 + (rows[j] >> 5) * 4), "r"(sw[j]) : "memory");
+        }
+    }
+}
+
+template <int BN, bool PAIR, bool QKV, bool F16, bool FUSE>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
-mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
-               const __grid_constant__ MxKernelParams p) {
-    using P = MxPlan<BN, PAIR>;
+mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ MxKernelParams p) {
+    using P = MxPlan<BN, PAIR, FUSE>;
     constexpr int NB = P::NB, STAGES = P::STAGES, ACC_BUFS = P::ACC_BUFS, STAGE_BYTES = P::STAGE_BYTES;
+    constexpr int CW = PAIR ? 128 : BN;  // columns of an epilogue warpgroup
+    constexpr bool SPLIT_REGS = QKV || CW == 128;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
+    const uint32_t ring = smem_base + P::RESIDENT;
     const uint32_t bar_base = smem_base + P::BAR_OFFSET;
     auto full_bar = [&](int s) { return bar_base + 8u * s; };
     auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
     auto sfready_bar = [&](int s) { return bar_base + 8u * (2 * STAGES + s); };
     auto tfull_bar = [&](int a) { return bar_base + 8u * (3 * STAGES + a); };
     auto tempty_bar = [&](int a) { return bar_base + 8u * (3 * STAGES + 2 + a); };
-    auto peer_bar = [&](int s) { return bar_base + 8u * (3 * STAGES + 4 + s); };  // pairs, leader: the other CTA's stage has landed
-    const uint32_t drain_bar = bar_base + 248u;  // see umma_drain
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_gen + P::BAR_OFFSET + 240);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + P::BAR_OFFSET + 244);
+    const uint32_t xready_bar = bar_base + 8u * (3 * STAGES + 4);                  // FUSE: the activations are in shared memory
+    auto peer_bar = [&](int s) { return bar_base + 8u * (3 * STAGES + 5 + s); };  // pairs, leader: the other CTA's stage has landed
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_gen + P::BAR_OFFSET + 480);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + P::BAR_OFFSET + 484);
+    const uint32_t drain_bar = bar_base + 488u;  // see umma_drain
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
@@ -306,10 +379,11 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             mbar_init(tfull_bar(a), 1);
             mbar_init(tempty_bar(a), PAIR ? 2 * NUM_EPI_WARPS * 32 : NUM_EPI_WARPS * 32 / 2);
         }
+        mbar_init(xready_bar, NUM_EPI_WARPS * 32);
         mbar_init(drain_bar, 1);
         *abort_flag = 0;
         fence_mbar_init();
-        tma_prefetch_desc(&tmap_a);
+        if constexpr (!FUSE) tma_prefetch_desc(&tmap_a);
         tma_prefetch_desc(&tmap_b);
     }
     if (warp == 1) {
@@ -326,124 +400,161 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
     if constexpr (PAIR) cluster_sync_all();  // the other CTA's barriers are initialised before anything arrives on them
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
-    grid_dependency_wait();  // everything above touched only this CTA's own shared and tensor memory
-    grid_launch_dependents();
+    // (everything above touched only this CTA's own shared and tensor memory; the warps that touch global memory wait for the previous
+    // kernel before they do)
 
     if (warp < 4) {
-    // With the norm and rotation an epilogue thread holds 32 values in transit beside the 128 it has read: 72 and 208 registers a thread
-    // (128 * 72 + 256 * 208 of the 384 * 168 at launch)
-    if constexpr (QKV) reg_dealloc<72>();
-    if (warp == 0) {
-        // ------------------------------------------------------------ producer
-        RingPos<STAGES> at;
-        bool ok = true;
-        for (int tile = tile_first; ok && tile < num_tiles; tile += tile_step) {
-            const int m_blk = (tile % num_m_blocks) * (PAIR ? 2 : 1) + static_cast<int>(cta_rank), n_blk = tile / num_m_blocks;
-            const int m0 = m_blk * BM, n0 = n_blk * BN + (PAIR ? static_cast<int>(cta_rank) * 128 : 0);
-            // (rows past M or N are filled with zeros and still counted; the atoms of 256 rows always exist)
-            const uint8_t* asf = p.asf + (static_cast<size_t>(m_blk >> 1) * p.nkb * 2 + (m_blk & 1)) * ATOMS;
-            const uint8_t* bsf = PAIR ? p.bsf + static_cast<size_t>(n_blk) * p.nkb * 2 * ATOMS
-                                      : p.bsf + (static_cast<size_t>(n_blk >> 1) * p.nkb * 2 + (n_blk & 1)) * ATOMS;
-            for (int kb = 0; kb < p.nkb; ++kb, at.next()) {
-                const uint32_t s = at.s;
-                if (!mbar_wait(empty_bar(s), at.ph ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER)) { ok = false; break; }
-                const uint32_t st = smem_base + s * STAGE_BYTES;
-                if (!elect_one()) continue;
-                mbar_arrive_expect_tx(full_bar(s), (p.a_box + p.b_box) * 128 + (1 + NB) * ATOMS);
-                tma_load_2d(st, &tmap_a, full_bar(s), kb * 128, m0);  // byte coordinates
-                tma_load_2d(st + A_BYTES, &tmap_b, full_bar(s), kb * 128, n0);
-                bulk_load(st + A_BYTES + P::B_BYTES, asf + static_cast<size_t>(kb) * 2 * ATOMS, ATOMS, full_bar(s));
-                bulk_load(st + A_BYTES + P::B_BYTES + ATOMS, bsf + static_cast<size_t>(kb) * 2 * ATOMS, NB * ATOMS, full_bar(s));
-            }
-        }
-        if (!ok && lane == 0) {  // a wait gave up: copies in flight land before the CTA leaves
-            const uint32_t first = at.it > STAGES ? at.it - STAGES : 0;
-            for (uint32_t j = first; j < at.it; ++j) {
-                const unsigned long long t0 = globaltimer_ns();
-                while (!mbar_try_wait(full_bar(j % STAGES), (j / STAGES) & 1) && globaltimer_ns() - t0 < 100000000ull) {}
-            }
-        }
-    } else if (warp == 1) {
-        // ------------------------------------------------------------ MMA issuer
-        if (cta_rank == 0) {
-            constexpr uint32_t idesc0 = mx_idesc(TILE_ROWS, BN, 0), idesc1 = mx_idesc(TILE_ROWS, BN, 1);
-            const uint64_t desc0 = umma_desc_sw128(smem_base);
+        // An epilogue thread holds 32 values in transit beside the 128 it has read: 72 and 208 registers a thread (128 * 72 + 256 * 208 of the
+        // 384 * 168 at launch)
+        if constexpr (SPLIT_REGS) reg_dealloc<72>();
+        if (warp == 0) {
+            // ------------------------------------------------------------ producer
             RingPos<STAGES> at;
-            uint32_t tcount = 0;
             bool ok = true;
-            for (int tile = tile_first; ok && tile < num_tiles; tile += tile_step, ++tcount) {
-                const uint32_t acc = tcount % ACC_BUFS;
-                if (!mbar_wait(tempty_bar(acc), ((tcount / ACC_BUFS) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_MMA)) { ok = false; break; }
-                tc_fence_after_sync();
-                const uint32_t d = tmem_base + acc * BN;
+            int early = 0;  // stages of the first tile whose rows of b are already on their way
+            auto load_a = [&](int m_blk, int kb, uint32_t st, uint32_t bar) {
+                tma_load_2d(st, &tmap_a, bar, kb * 128, m_blk * BM);  // byte coordinates; rows past M are filled with zeros and still counted
+                bulk_load(st + P::SF_OFFSET, p.asf + ((static_cast<size_t>(m_blk >> 1) * p.nkb + kb) * 2 + (m_blk & 1)) * ATOMS, ATOMS, bar);
+            };
+            auto load_b = [&](int n_blk, int kb, uint32_t st, uint32_t bar) {
+                tma_load_2d(st + P::A_STAGE, &tmap_b, bar, kb * 128, n_blk * BN + (PAIR ? static_cast<int>(cta_rank) * 128 : 0));
+                const int rb = n_blk * BN / 128;  // (the atoms of 256 rows always exist)
+                bulk_load(st + P::SFB_OFFSET, p.bsf + ((static_cast<size_t>(rb >> 1) * p.nkb + kb) * 2 + (rb & 1)) * ATOMS, NB * ATOMS, bar);
+            };
+            const uint32_t stage_tx = ((FUSE ? 0 : p.a_box) + p.b_box) * 128 + (NB + (FUSE ? 0 : 1)) * ATOMS;
+            if (!FUSE && p.early && tile_first < num_tiles) {
+                // the previous kernel is this call's own quantizer, which does not write b: b's first stages land while it runs
+                early = min(STAGES, p.nkb);
+                if (elect_one())
+                    for (int kb = 0; kb < early; ++kb) {
+                        mbar_arrive_expect_tx(full_bar(kb), stage_tx);
+                        load_b(tile_first / num_m_blocks, kb, ring + kb * STAGE_BYTES, full_bar(kb));
+                    }
+                __syncwarp();
+            }
+            grid_dependency_wait();
+            for (int tile = tile_first; ok && tile < num_tiles; tile += tile_step) {
+                const int m_blk = (tile % num_m_blocks) * (PAIR ? 2 : 1) + static_cast<int>(cta_rank), n_blk = tile / num_m_blocks;
                 for (int kb = 0; kb < p.nkb; ++kb, at.next()) {
                     const uint32_t s = at.s;
-                    // (the copier warps have seen the stage's loads land, in both CTAs of a pair: their barrier covers the operands)
-                    if (!mbar_wait(sfready_bar(s), at.ph, abort_flag, p.status, DEV_TIMEOUT_MMA)) { ok = false; break; }
-                    tc_fence_after_sync();
-                    const uint32_t tsf = tmem_base + P::TMEM_SF + s * P::SF_COLS;
-                    const uint64_t adesc = desc0 + s * (STAGE_BYTES >> 4), bdesc = adesc + (A_BYTES >> 4);
+                    if (!mbar_wait(empty_bar(s), at.ph ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER)) { ok = false; break; }
+                    const uint32_t st = ring + s * STAGE_BYTES;
                     if (!elect_one()) continue;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)  // K = 64 elements = 32 bytes per instruction
-                        umma_mxf4<PAIR>(d, adesc + 2 * k, bdesc + 2 * k, (k & 1) ? idesc1 : idesc0, tsf + 4 * (k >> 1), tsf + 8 + 4 * NB * (k >> 1),
-                                        (kb | k) != 0);
-                    if constexpr (PAIR) umma_commit_pair(empty_bar(s), 3);
-                    else umma_commit(empty_bar(s));
-                }
-                if (ok && elect_one()) {
-                    if constexpr (PAIR) umma_commit_pair(tfull_bar(acc), 3);
-                    else umma_commit(tfull_bar(acc));
-                }
-            }
-        }
-    } else {
-        // ------------------------------------------------------------ scale copiers
-        RingPos<STAGES> at;
-        bool ok = true;
-        for (int tile = tile_first; ok && tile < num_tiles; tile += tile_step) {
-            for (int kb = 0; kb < p.nkb; ++kb, at.next()) {
-                const uint32_t s = at.s;
-                if (!mbar_wait(full_bar(s), at.ph, abort_flag, p.status, DEV_TIMEOUT_UNPACK)) { ok = false; break; }
-                if constexpr (PAIR) {
-                    if (cta_rank != 0) {  // this CTA's stage has landed: the leader acts for both
-                        if (warp == 2 && elect_one()) mbar_arrive_cluster(map_to_cta(peer_bar(s), 0));
-                        continue;
+                    const bool begun = !FUSE && static_cast<int>(at.it) < early;
+                    if (!begun) {
+                        mbar_arrive_expect_tx(full_bar(s), stage_tx);
+                        load_b(n_blk, kb, st, full_bar(s));
                     }
-                    if (!mbar_wait(peer_bar(s), at.ph, abort_flag, p.status, DEV_TIMEOUT_UNPACK)) { ok = false; break; }
+                    if constexpr (!FUSE) load_a(m_blk, kb, st, full_bar(s));
                 }
-                tc_fence_after_sync();
-                const uint32_t sf = smem_base + s * STAGE_BYTES + A_BYTES + P::B_BYTES;
-                const uint32_t tsf = tmem_base + P::TMEM_SF + s * P::SF_COLS;
-                if (!elect_one()) continue;
-                // atom i of a at column 4 i; atom i of column block b at 8 + 4 NB i + 4 b (the blocks of a tile side by side)
-                if (warp == 2) {
-                    sf_copy<PAIR>(tsf, sf_desc(sf));
-                    sf_copy<PAIR>(tsf + 4, sf_desc(sf + 512));
-                    if constexpr (NB == 2) sf_copy<PAIR>(tsf + 8, sf_desc(sf + ATOMS));
-                } else {
-                    if constexpr (NB == 1) sf_copy<PAIR>(tsf + 8, sf_desc(sf + ATOMS));
-                    if constexpr (NB == 2) sf_copy<PAIR>(tsf + 12, sf_desc(sf + 2 * ATOMS));
+            }
+            if (!ok && lane == 0) {  // a wait gave up: copies in flight land before the CTA leaves
+                const uint32_t first = at.it > STAGES ? at.it - STAGES : 0;
+                for (uint32_t j = first; j < at.it; ++j) {
+                    const unsigned long long t0 = globaltimer_ns();
+                    while (!mbar_try_wait(full_bar(j % STAGES), (j / STAGES) & 1) && globaltimer_ns() - t0 < 100000000ull) {}
+                }
+            }
+        } else if (warp == 1) {
+            // ------------------------------------------------------------ MMA issuer
+            if (cta_rank == 0) {
+                constexpr uint32_t idesc0 = mx_idesc(TILE_ROWS, BN, 0), idesc1 = mx_idesc(TILE_ROWS, BN, 1);
+                const uint64_t desc0 = umma_desc_sw128(ring);
+                const uint64_t xdesc = umma_desc_sw128(smem_base);  // FUSE: the resident codes
+                RingPos<STAGES> at;
+                uint32_t tcount = 0;
+                bool ok = true;
+                if constexpr (FUSE) ok = mbar_wait(xready_bar, 0, abort_flag, p.status, DEV_TIMEOUT_MMA);
+                for (int tile = tile_first; ok && tile < num_tiles; tile += tile_step, ++tcount) {
+                    const uint32_t acc = tcount % ACC_BUFS;
+                    if (!mbar_wait(tempty_bar(acc), ((tcount / ACC_BUFS) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_MMA)) { ok = false; break; }
+                    tc_fence_after_sync();
+                    const uint32_t d = tmem_base + acc * BN;
+                    // a 64-column tile's scales are one half of its 128-column block's: rows 0..63 lie in an atom's first two columns of tensor memory
+                    const uint32_t half = BN == 64 ? 2 * ((tile / num_m_blocks) & 1) : 0;
+                    for (int kb = 0; kb < p.nkb; ++kb, at.next()) {
+                        const uint32_t s = at.s;
+                        // (the copier warps have seen the stage's loads land, in both CTAs of a pair: their barrier covers the operands)
+                        if (!mbar_wait(sfready_bar(s), at.ph, abort_flag, p.status, DEV_TIMEOUT_MMA)) { ok = false; break; }
+                        tc_fence_after_sync();
+                        const uint32_t tsf = tmem_base + P::TMEM_SF + s * P::SF_COLS;
+                        const uint64_t sdesc = desc0 + s * (STAGE_BYTES >> 4);
+                        const uint64_t adesc = FUSE ? xdesc + static_cast<uint32_t>(kb * p.groups * (1024 >> 4)) : sdesc;
+                        const uint64_t bdesc = sdesc + (P::A_STAGE >> 4);
+                        if (!elect_one()) continue;
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) sf_copy<PAIR>(tsf + 8 + 4 * NB + 4 * b, sf_desc(sf + (1 + b) * ATOMS + 512));
+                        for (int k = 0; k < 4; ++k)  // K = 64 elements = 32 bytes per instruction
+                            umma_mxf4<PAIR>(d, adesc + 2 * k, bdesc + 2 * k, (k & 1) ? idesc1 : idesc0, tsf + 4 * (k >> 1), tsf + 8 + 4 * NB * (k >> 1) + half,
+                                            (kb | k) != 0);
+                        if constexpr (PAIR) umma_commit_pair(empty_bar(s), 3);
+                        else umma_commit(empty_bar(s));
+                    }
+                    if (ok && elect_one()) {
+                        if constexpr (PAIR) umma_commit_pair(tfull_bar(acc), 3);
+                        else umma_commit(tfull_bar(acc));
+                    }
                 }
-                if constexpr (PAIR) umma_commit_pair(sfready_bar(s), 1);  // the leader's barrier only
-                else umma_commit(sfready_bar(s));
+            }
+        } else {
+            // ------------------------------------------------------------ scale copiers
+            RingPos<STAGES> at;
+            bool ok = true;
+            if constexpr (FUSE) ok = mbar_wait(xready_bar, 0, abort_flag, p.status, DEV_TIMEOUT_UNPACK);
+            for (int tile = tile_first; ok && tile < num_tiles; tile += tile_step) {
+                for (int kb = 0; kb < p.nkb; ++kb, at.next()) {
+                    const uint32_t s = at.s;
+                    if (!mbar_wait(full_bar(s), at.ph, abort_flag, p.status, DEV_TIMEOUT_UNPACK)) { ok = false; break; }
+                    if constexpr (PAIR) {
+                        if (cta_rank != 0) {  // this CTA's stage has landed: the leader acts for both
+                            if (warp == 2 && elect_one()) mbar_arrive_cluster(map_to_cta(peer_bar(s), 0));
+                            continue;
+                        }
+                        if (!mbar_wait(peer_bar(s), at.ph, abort_flag, p.status, DEV_TIMEOUT_UNPACK)) { ok = false; break; }
+                    }
+                    tc_fence_after_sync();
+                    const uint32_t sfa = FUSE ? smem_base + p.nkb * p.groups * 1024 + kb * ATOMS : ring + s * STAGE_BYTES + P::SF_OFFSET;
+                    const uint32_t sfb = ring + s * STAGE_BYTES + P::SFB_OFFSET;
+                    const uint32_t tsf = tmem_base + P::TMEM_SF + s * P::SF_COLS;
+                    if (!elect_one()) continue;
+                    // atom i of a at column 4 i; atom i of column block b at 8 + 4 NB i + 4 b (the blocks of a tile side by side)
+                    if (warp == 2) {
+                        sf_copy<PAIR>(tsf, sf_desc(sfa));
+                        sf_copy<PAIR>(tsf + 4, sf_desc(sfa + 512));
+                        if constexpr (NB == 2) sf_copy<PAIR>(tsf + 8, sf_desc(sfb));
+                    } else {
+                        if constexpr (NB == 1) sf_copy<PAIR>(tsf + 8, sf_desc(sfb));
+                        if constexpr (NB == 2) sf_copy<PAIR>(tsf + 12, sf_desc(sfb + ATOMS));
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) sf_copy<PAIR>(tsf + 8 + 4 * NB + 4 * b, sf_desc(sfb + b * ATOMS + 512));
+                    }
+                    if constexpr (PAIR) umma_commit_pair(sfready_bar(s), 1);  // the leader's barrier only
+                    else umma_commit(sfready_bar(s));
+                }
             }
         }
-    }
     } else {
         // ------------------------------------------------------------ epilogue
-        if constexpr (QKV) reg_alloc<208>();
-        // warp % 4 selects the quadrant of tensor-memory lanes (32 rows); a warpgroup has 128 columns: half of a pair's tile, or the whole of
-        // every second 128-column tile.  A warp reads its 32 x 128 values and hands the accumulator back before it converts them.
+        // warp % 4 selects the quadrant of tensor-memory lanes (32 rows); a warpgroup has CW columns: half of a pair's tile, or the whole of every
+        // second tile.  A warp reads its 32 x CW values and hands the accumulator back before it converts them.
         //
-        // Loads of 16 lanes x 256 bits leave lane l with columns 8 J + 2 t, + 1 (t = l % 4, J = 0..15) of rows l / 4 + 8 i (i = 0..3): exchanged within
-        // the four lanes of a row (transpose4), each lane has four runs of 8 consecutive columns, 32 m + 8 t, of its four rows, 64 bytes of a
-        // row side by side in a store.  (Through shared memory and TMA stores instead: the same time at K = 12288, and 32 KB that hold a
-        // stage of operands here.)
+        // Loads of 16 lanes x 256 bits leave lane l with columns 8 J + 2 t, + 1 (t = l % 4) of rows l / 4 + 8 i (i = 0..3): exchanged within the four
+        // lanes of a row (transpose4), each lane has runs of 8 consecutive columns, 32 m + 8 t, of its four rows, 64 bytes of a row side by side
+        // in a store.  (Through shared memory and TMA stores instead: the same time at K = 12288, and 32 KB that hold a stage of operands
+        // here.)
+        if constexpr (SPLIT_REGS) reg_alloc<208>();
+        constexpr int RUNS = CW / 32, CH = CW / 64;
         const int q = warp & 3, group = (warp - 4) >> 2, gt = threadIdx.x & 127;
         const int t = lane & 3, r4 = lane >> 2;
+        grid_dependency_wait();
+        grid_launch_dependents();  // the next kernel may be scheduled as this grid's CTAs leave (it waits for this whole grid)
+        if constexpr (FUSE) {
+            const uint32_t sfa = smem_base + p.nkb * p.groups * 1024;
+            if (p.x_dtype == DIROTQ_DTYPE_BF16) quantize_resident<__nv_bfloat16>(p, smem_base, sfa, warp - 4, lane);
+            else if (p.x_dtype == DIROTQ_DTYPE_F16) quantize_resident<__half>(p, smem_base, sfa, warp - 4, lane);
+            else quantize_resident<float>(p, smem_base, sfa, warp - 4, lane);
+            fence_proxy_async_smem();  // these writes -> visible to the tensor core
+            mbar_arrive(xready_bar);
+        }
         float* s_hw = reinterpret_cast<float*>(smem_gen + P::HEADW_OFFSET);
         if constexpr (QKV) {  // (both warpgroups write the same values; each reads behind its own barrier below)
             const int i = gt & ((1 << p.head_shift) - 1);
@@ -458,108 +569,139 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             // the bias of these columns goes to shared memory while the tile's MMAs run (two buffers: a warp can be a tile ahead); the
             // barrier orders the stores before the reads and makes the warpgroup agree on whether to go on
             float* s_b = reinterpret_cast<float*>(smem_gen + P::BIAS_OFFSET) + (group * 2 + (use & 1)) * 128;
-            s_b[gt] = p.bias != nullptr && n0 + gt < p.N ? load_16(p.bias, n0 + gt, p.f16) : 0.f;
+            if (gt < CW) s_b[gt] = p.bias != nullptr && n0 + gt < p.N ? load_16(p.bias, n0 + gt, F16) : 0.f;
             const bool failed = !mbar_wait(tfull_bar(acc), use & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
             if (group == 0 ? group_any<1>(failed) : group_any<2>(failed)) break;
             tc_fence_after_sync();
             const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * BN + (PAIR ? group * 128 : 0);
-            uint32_t raw[2][2][32];  // [rows 16 h ..][columns 64 c ..][4 j + 2 (row + 8) + (column + 1)], J = 8 c + j
+            uint32_t raw[2][CH][32];  // [rows 16 h ..][columns 64 c ..][4 j + 2 (row + 8) + (column + 1)], J = 8 c + j
             const bool stored = row0 < p.M && n0 < p.N;  // (uniform in the warp)
             if (stored) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) tmem_ld_16x256b_x8(taddr + (static_cast<uint32_t>(16 * h) << 16) + c * 64, raw[h][c]);
+                    for (int c = 0; c < CH; ++c) tmem_ld_16x256b_x8(taddr + (static_cast<uint32_t>(16 * h) << 16) + c * 64, raw[h][c]);
                 tmem_ld_wait();
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) tmem_ld_fence(raw[h][c]);
+                    for (int c = 0; c < CH; ++c) tmem_ld_fence(raw[h][c]);
             }
             tc_fence_before_sync();
             if constexpr (PAIR) mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));  // the leader's barrier
             else mbar_arrive(tempty_bar(acc));
             if (!stored) continue;
+
+            // the rows l / 4 + 8 i of the tile's columns, i = 2 h + hi (of registers that hold h in place 0), rounded and exchanged
+            auto convert = [&](const uint32_t (&src)[CH][32], int hi, uint4 (&out)[RUNS]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (row0 + 8 * i >= p.M) break;
-                const int row = row0 + 8 * i + r4;
-                uint4 out[4];
-                if (QKV && n0 < p.k_end) {
-                    float v[4][8];  // columns 32 m + 8 t + e
+                for (int m = 0; m < RUNS; ++m) {
+                    uint32_t w[4];
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        uint32_t lo[4], hi[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            lo[k] = raw[i >> 1][m >> 1][16 * (m & 1) + 4 * k + 2 * (i & 1)];
-                            hi[k] = raw[i >> 1][m >> 1][16 * (m & 1) + 4 * k + 2 * (i & 1) + 1];
-                        }
-                        transpose4(lo, t);
-                        transpose4(hi, t);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float2 b = *reinterpret_cast<const float2*>(s_b + 32 * m + 8 * t + 2 * k);
-                            v[m][2 * k] = __uint_as_float(lo[k]) + b.x;
-                            v[m][2 * k + 1] = __uint_as_float(hi[k]) + b.y;
-                        }
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 b = *reinterpret_cast<const float2*>(s_b + 32 * m + 8 * k + 2 * t);
+                        w[k] = pack2<F16>(__uint_as_float(src[m >> 1][16 * (m & 1) + 4 * k + 2 * hi]) + b.x,
+                                          __uint_as_float(src[m >> 1][16 * (m & 1) + 4 * k + 2 * hi + 1]) + b.y);
                     }
-                    int pos = row;
-                    if (p.positions != nullptr && row < p.M) pos = __ldg(p.positions + row);
-                    const bool turned = row < p.M && (p.rope == DIROTQ_ROPE_NONE || (pos >= 0 && pos < p.num_positions));
-                    if (!turned) pos = 0;
-                    if (p.head_shift == 7) head_norm_rope<4>(v, turned, s_hw + (n0 < p.q_cols ? 0 : 128), t, pos, p);
-                    else {
-                        head_norm_rope<2>(v, turned, s_hw + (n0 < p.q_cols ? 0 : 128), t, pos, p);
-                        head_norm_rope<2>(v + 2, turned && n0 + 64 < p.k_end, s_hw + (n0 + 64 < p.q_cols ? 0 : 128), t, pos, p);
-                    }
-#pragma unroll
-                    for (int m = 0; m < 4; ++m)
-                        out[m] = make_uint4(pack2(v[m][0], v[m][1], p.f16), pack2(v[m][2], v[m][3], p.f16), pack2(v[m][4], v[m][5], p.f16),
-                                            pack2(v[m][6], v[m][7], p.f16));
-                } else {
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float2 b = *reinterpret_cast<const float2*>(s_b + 32 * m + 8 * k + 2 * t);
-                            w[k] = pack2(__uint_as_float(raw[i >> 1][m >> 1][16 * (m & 1) + 4 * k + 2 * (i & 1)]) + b.x,
-                                         __uint_as_float(raw[i >> 1][m >> 1][16 * (m & 1) + 4 * k + 2 * (i & 1) + 1]) + b.y, p.f16);
-                        }
-                        transpose4(w, t);
-                        out[m] = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
+                    transpose4(w, t);
+                    out[m] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                uint16_t* yrow = reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row) * p.ldy + n0;
-                if (p.wide_out && n0 + 128 <= p.N) {
+            };
+            uint16_t* ytile = reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row0) * p.ldy + n0;
+            const bool whole = p.wide_out && n0 + CW <= p.N;
+            if (!QKV && whole && row0 + 32 <= p.M) {
 #pragma unroll
-                    for (int m = 0; m < 4; ++m)
-                        if (row < p.M) *reinterpret_cast<uint4*>(yrow + 32 * m + 8 * t) = out[m];
-                } else {
-                    // ragged or unaligned rows: through 1 KB of shared memory, 64 columns at a time, written by consecutive lanes
-                    const uint32_t edge = smem_base + P::EDGE_OFFSET + static_cast<uint32_t>(warp - 4) * 1024u;
-                    uint16_t* ytop = reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row0 + 8 * i) * p.ldy + n0;
-                    const int rows = min(8, p.M - row0 - 8 * i);
+                for (int i = 0; i < 4; ++i) {
+                    uint4 out[RUNS];
+                    convert(raw[i >> 1], i & 1, out);
+                    uint16_t* yrow = ytile + (8 * i + r4) * p.ldy + 8 * t;
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        __syncwarp();
+                    for (int m = 0; m < RUNS; ++m) __stcs(reinterpret_cast<uint4*>(yrow + 32 * m), out[m]);
+                }
+                continue;
+            }
+            // Heads, ragged and unaligned tiles.  The loop over the 16-row halves is kept rolled (the second half's registers move into the first's
+            // place): unrolled, its code is fetched for longer than it runs in short calls (64 tokens of q/k/v 14.5 against 13.1 us, 4608
+            // tokens 90 against 84).
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                        for (int m = 0; m < 2; ++m)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(edge + r4 * 128 + m * 64 + t * 16), "r"(out[2 * c + m].x),
-                                         "r"(out[2 * c + m].y), "r"(out[2 * c + m].z), "r"(out[2 * c + m].w)
-                                         : "memory");
-                        __syncwarp();
-                        for (int r = 0; r < rows; ++r)
+                for (int hi = 0; hi < 2; ++hi) {
+                    const int first = 16 * h + 8 * hi;  // of the eight rows
+                    if (row0 + first >= p.M) continue;
+                    const int row = row0 + first + r4;
+                    uint4 out[RUNS];
+                    if (QKV && n0 < p.k_end) {
+                        float v[RUNS][8];  // columns 32 m + 8 t + e
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const int col = c * 64 + 32 * h + lane;
-                                uint16_t e;
-                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(e) : "r"(edge + r * 128 + 64 * h + 2 * lane) : "memory");
-                                if (n0 + col < p.N) ytop[r * p.ldy + col] = e;
+                        for (int m = 0; m < RUNS; ++m) {
+                            uint32_t even[4], odd[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                even[k] = raw[0][m >> 1][16 * (m & 1) + 4 * k + 2 * hi];
+                                odd[k] = raw[0][m >> 1][16 * (m & 1) + 4 * k + 2 * hi + 1];
                             }
+                            transpose4(even, t);
+                            transpose4(odd, t);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const float2 b = *reinterpret_cast<const float2*>(s_b + 32 * m + 8 * t + 2 * k);
+                                v[m][2 * k] = __uint_as_float(even[k]) + b.x;
+                                v[m][2 * k + 1] = __uint_as_float(odd[k]) + b.y;
+                            }
+                        }
+                        int pos = row;
+                        if (p.positions != nullptr && row < p.M) pos = __ldg(p.positions + row);
+                        const bool turned = row < p.M && (p.rope == DIROTQ_ROPE_NONE || (pos >= 0 && pos < p.num_positions));
+                        if (!turned) pos = 0;
+                        if (RUNS == 4 && p.head_shift == 7) {
+                            head_norm_rope<RUNS>(v, turned, s_hw + (n0 < p.q_cols ? 0 : 128), t, pos, p);
+                        } else {
+#pragma unroll
+                            for (int m = 0; m < RUNS; m += 2)
+                                head_norm_rope<2>(v + m, turned && n0 + 32 * m < p.k_end, s_hw + (n0 + 32 * m < p.q_cols ? 0 : 128), t, pos, p);
+                        }
+#pragma unroll
+                        for (int m = 0; m < RUNS; ++m)
+                            out[m] = make_uint4(pack2<F16>(v[m][0], v[m][1]), pack2<F16>(v[m][2], v[m][3]), pack2<F16>(v[m][4], v[m][5]),
+                                                pack2<F16>(v[m][6], v[m][7]));
+                    } else {
+                        convert(raw[0], hi, out);
+                    }
+                    uint16_t* yrows = ytile + first * p.ldy;
+                    if (whole) {
+#pragma unroll
+                        for (int m = 0; m < RUNS; ++m)
+                            if (row < p.M) *reinterpret_cast<uint4*>(yrows + r4 * p.ldy + 32 * m + 8 * t) = out[m];
+                    } else {
+                        // through 1 KB of shared memory, 64 columns at a time, written by consecutive lanes
+                        const uint32_t edge = smem_base + P::EDGE_OFFSET + static_cast<uint32_t>(warp - 4) * 1024u;
+                        const int rows = min(8, p.M - row0 - first);
+#pragma unroll
+                        for (int c = 0; c < CH; ++c) {
+                            __syncwarp();
+#pragma unroll
+                            for (int m = 0; m < 2; ++m)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(edge + r4 * 128 + m * 64 + t * 16), "r"(out[2 * c + m].x),
+                                             "r"(out[2 * c + m].y), "r"(out[2 * c + m].z), "r"(out[2 * c + m].w)
+                                             : "memory");
+                            __syncwarp();
+#pragma unroll 1
+                            for (int r = 0; r < rows; ++r)
+#pragma unroll
+                                for (int g = 0; g < 2; ++g) {
+                                    const int col = c * 64 + 32 * g + lane;
+                                    uint16_t e;
+                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(e) : "r"(edge + r * 128 + 64 * g + 2 * lane) : "memory");
+                                    if (n0 + col < p.N) yrows[r * p.ldy + col] = e;
+                                }
+                        }
                     }
                 }
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) raw[0][c][j] = raw[1][c][j];
             }
         }
     }
@@ -583,42 +725,99 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
     }
 }
 
-template <int BN, bool PAIR, bool QKV>
-dirotq_status_t launch_plan(const MxGemmArgs& a, const MxKernelParams& p, cudaStream_t stream) {
-    using P = MxPlan<BN, PAIR>;
-    auto kern = mx_gemm_kernel<BN, PAIR, QKV>;
+template <int BN, bool PAIR, bool QKV, bool F16, bool FUSE>
+dirotq_status_t launch_kernel_of(const MxGemmArgs& a, MxKernelParams& p, cudaStream_t stream) {
+    using P = MxPlan<BN, PAIR, FUSE>;
+    auto kern = mx_gemm_kernel<BN, PAIR, QKV, F16, FUSE>;
     const int device = a.b->device, sms = sm_count(device);
     static SmemOptIn<1> opt_in;
     if (!opt_in.ensure(kern, 0, device, P::SMEM_BYTES)) return DIROTQ_ERR_CUDA;
     const long long rows = PAIR ? 2 * BM : BM;
     const long long tiles = (p.M + rows - 1) / rows * ((p.N + BN - 1) / BN);
+    const CUtensorMap& tmap_b = BN == 64 ? a.b->tmap64 : a.b->tmap;
+    const CUtensorMap& tmap_a = FUSE ? tmap_b : a.a->tmap;  // (not used when the activations are quantized here)
+    p.b_box = BN == 64 ? a.b->box64 : a.b->box;
     cudaError_t err;
     if constexpr (PAIR) {
         const int pairs = static_cast<int>(tiles < sms / 2 ? tiles : sms / 2);
-        err = launch_kernel_pairs(kern, 2 * pairs, NUM_THREADS, P::SMEM_BYTES, stream, true, a.a->tmap, a.b->tmap, p);
+        err = launch_kernel_pairs(kern, 2 * pairs, NUM_THREADS, P::SMEM_BYTES, stream, true, tmap_a, tmap_b, p);
     } else {
-        err = launch_kernel(kern, static_cast<int>(tiles < sms ? tiles : sms), NUM_THREADS, P::SMEM_BYTES, stream, true, a.a->tmap, a.b->tmap, p);
+        err = launch_kernel(kern, static_cast<int>(tiles < sms ? tiles : sms), NUM_THREADS, P::SMEM_BYTES, stream, true, tmap_a, tmap_b, p);
     }
     if (err != cudaSuccess) set_error("mx_gemm_kernel", err);
     return err == cudaSuccess ? DIROTQ_OK : DIROTQ_ERR_CUDA;
 }
 
+template <int BN, bool PAIR, bool FUSE>
+dirotq_status_t launch_plan(const MxGemmArgs& a, MxKernelParams& p, cudaStream_t stream) {
+    if (a.qk)
+        return a.y_dtype == DIROTQ_DTYPE_F16 ? launch_kernel_of<BN, PAIR, true, true, FUSE>(a, p, stream)
+                                             : launch_kernel_of<BN, PAIR, true, false, FUSE>(a, p, stream);
+    return a.y_dtype == DIROTQ_DTYPE_F16 ? launch_kernel_of<BN, PAIR, false, true, FUSE>(a, p, stream)
+                                         : launch_kernel_of<BN, PAIR, false, false, FUSE>(a, p, stream);
+}
+
+std::atomic<int> g_mx_tile{0};  // 0: chosen per call; 64 / 128: single CTAs with that many columns; 512: CTA pairs
+
+// Up to kFuseUnits units (256 elements of a row) the activations are quantized by the product's own CTAs (see FUSE): that takes about 0.3 us per
+// unit and warp there, a quantizer of its own about 1.5 us.  (K = 3072 -> 9216: 2 rows, 24 units, 6.1 against 6.6 us, 4 rows 7.1; 1152 -> 1152: 6 rows, 30
+// units, 4.7 against 5.5, 8 rows 5.2, 12 rows 6.3; 12288 -> 3072: 1 row, 48 units, 12.6 against 12.1.)
+constexpr int kFuseUnits = 32;
+template <int BN>
+bool fuse_fits(int M, int nkb) {
+    return static_cast<long long>(M) * nkb <= kFuseUnits && M <= 32 && nkb * ((M + 7) / 8 + 1) * 1024 <= MxPlan<BN, false, true>::RESIDENT;
+}
+
+// Columns per tile of single CTAs, or 512 for pairs: the shortest schedule, turns of the SMs x the time of a tile.  Microseconds a tile of nkb
+// k-blocks takes, from calls of one to nine turns: 64 columns 0.30 + 0.17 nkb, 128 columns 0.55 + 0.235 nkb, pairs 1.0 + 0.36 nkb and 1.3
+// once (clusters start later).  (512 rows, K 1152 -> 1152: 3.5, 4.4, 6.2 us; 512 rows, 3072 -> 9216: 11.9, 9.2, 9.6; 4608 rows: pairs 50.)
+int choose_plan(int M, int N, int nkb, const dirotq_qk_t* qk, int sms) {
+    const bool heads_of_128 = qk != nullptr && qk->head_dim == 128;  // (a tile's columns are whole heads)
+    const int forced = g_mx_tile.load();
+    if (forced != 0 && !(forced == 64 && heads_of_128)) return forced;
+    auto turns = [](long long tiles, int units) { return static_cast<double>((tiles + units - 1) / units); };
+    const long long mb = (M + BM - 1) / BM;
+    const double t64 = heads_of_128 ? 1e30 : turns(mb * ((N + 63) / 64), sms) * (0.30 + 0.17 * nkb);
+    const double t128 = turns(mb * ((N + 127) / 128), sms) * (0.55 + 0.235 * nkb);
+    const double tpair = M <= BM ? 1e30 : 1.3 + turns((M + 2 * BM - 1) / (2 * BM) * ((N + 255ll) / 256), sms / 2) * (1.0 + 0.36 * nkb);
+    return tpair < t64 && tpair < t128 ? 512 : t128 < t64 ? 128 : 64;
+}
+
 }  // namespace
+
+dirotq_status_t set_mx_tile_columns(int columns) {
+    if (columns != 0 && columns != 64 && columns != 128 && columns != 512) return DIROTQ_ERR_INVALID_ARG;
+    g_mx_tile.store(columns);
+    return DIROTQ_OK;
+}
+
+bool mx_fuses(int M, int N, int nkb, const dirotq_qk_t* qk, int device) {
+    const int plan = choose_plan(M, N, nkb, qk, sm_count(device));
+    return plan == 64 ? fuse_fits<64>(M, nkb) : plan == 128 ? fuse_fits<128>(M, nkb) : false;
+}
 
 dirotq_status_t launch_mx_gemm(const MxGemmArgs& a, cudaStream_t stream) {
     MxKernelParams p = {};
-    p.M = a.a->rows;
+    p.M = a.M;
     p.N = a.b->rows;
-    p.nkb = a.a->lay.nkb;
-    p.a_box = a.a->box;
-    p.b_box = a.b->box;
-    p.asf = reinterpret_cast<const uint8_t*>(a.a->buffer) + a.a->lay.off_scales;
+    p.nkb = a.b->lay.nkb;
+    if (a.a) {
+        p.a_box = a.a->box;
+        p.asf = reinterpret_cast<const uint8_t*>(a.a->buffer) + a.a->lay.off_scales;
+    } else {
+        p.x = a.x;
+        p.ldx = a.ldx;
+        p.x_dtype = a.x_dtype;
+        p.x_wide = (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && a.ldx * static_cast<long long>(dtype_size(a.x_dtype)) % 16 == 0;
+        p.K = a.b->K;
+        p.scale_rule = a.scale_rule;
+        p.groups = (a.M + 7) / 8;
+    }
     p.bsf = reinterpret_cast<const uint8_t*>(a.b->buffer) + a.b->lay.off_scales;
     p.bias = a.bias;
     p.y = static_cast<uint8_t*>(a.y);
     p.ldy = a.ldy;
     p.status = a.status;
-    p.f16 = a.y_dtype == DIROTQ_DTYPE_F16;
     p.early = a.early_weights;
     p.wide_out = (reinterpret_cast<uintptr_t>(a.y) & 15u) == 0 && a.ldy % 8 == 0;
     if (a.qk) {
@@ -640,9 +839,11 @@ dirotq_status_t launch_mx_gemm(const MxGemmArgs& a, cudaStream_t stream) {
         p.num_positions = qk.num_positions;
         p.positions = qk.positions;
     }
-    // CTA pairs above 128 rows, where a second row block exists
-    if (p.M > BM) return a.qk ? launch_plan<256, true, true>(a, p, stream) : launch_plan<256, true, false>(a, p, stream);
-    return a.qk ? launch_plan<128, false, true>(a, p, stream) : launch_plan<128, false, false>(a, p, stream);
+    const int plan = choose_plan(p.M, p.N, p.nkb, a.qk, sm_count(a.b->device));
+    if (a.a == nullptr) return plan == 64 ? launch_plan<64, false, true>(a, p, stream) : launch_plan<128, false, true>(a, p, stream);
+    return plan == 512   ? launch_plan<256, true, false>(a, p, stream)
+           : plan == 128 ? launch_plan<128, false, false>(a, p, stream)
+                         : launch_plan<64, false, false>(a, p, stream);
 }
 
 }  // namespace dirotq

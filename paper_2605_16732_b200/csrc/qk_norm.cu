@@ -1,9 +1,8 @@
 // RMS norm of every head of q and k and the rotation by the token's position, in one pass over the output of a fused q/k/v projection.
 //
-// A group of LANES lanes (the power of two that covers head_dim at eight elements per lane) holds one head: the sum of squares is a few
-// shuffles, pairs (2i, 2i+1) lie in one lane, and the partner half a rotation away is fetched from the lane that holds it, or through shared
-// memory where the halves do not fall on whole lanes.  A block of threads serves one token, so that its cosines and sines are read once per
-// lane and kept for all of the lane's heads.
+// Memory sets the time: 4 bytes a value in 16 bits, and the tables.  head_dim / 8 lanes hold a head, eight consecutive elements each, so a warp
+// holds 32 / (head_dim / 8) whole heads side by side in memory; it takes kHeads such sets of one token's q, k or v at once, their loads in
+// flight together, with the token's cosines and sines kept in registers for all of them.  The sum of squares is a few shuffles.
 #include "mxfp4.cuh"
 #include "ptx.cuh"
 
@@ -32,7 +31,39 @@ struct QkParams {
     const int32_t* slots;
     int num_slots;
     int copy_v;
+    int wide_table;              // rows of both tables are 16-byte aligned
+    // how a warp's lanes are used: lanes of a head, heads side by side, the first step of the sum over L lanes, sets of a turn, turns
+    // of a token, of all
+    int L, per_warp, fold, part_sets, parts_q, parts_k, parts, items;
 };
+
+// Elements d0 .. + 3 and d1 .. + 3 of a head; SPLIT: two pieces (8 bytes each in 16 bits), else one (d1 = d0 + 4).
+template <typename T, bool SPLIT_PIECES>
+__device__ __forceinline__ Raw8<T> load_pieces(const T* head, int d0, int d1) {
+    Raw8<T> r;
+    if constexpr (sizeof(T) == 4) {
+        r.u[0] = *reinterpret_cast<const uint4*>(head + d0);
+        r.u[1] = *reinterpret_cast<const uint4*>(head + d1);
+    } else if constexpr (SPLIT_PIECES) {
+        const uint2 a = *reinterpret_cast<const uint2*>(head + d0), b = *reinterpret_cast<const uint2*>(head + d1);
+        r.u[0] = make_uint4(a.x, a.y, b.x, b.y);
+    } else {
+        r.u[0] = *reinterpret_cast<const uint4*>(head + d0);
+    }
+    return r;
+}
+template <typename T, bool SPLIT_PIECES>
+__device__ __forceinline__ void store_pieces(T* head, int d0, int d1, const Raw8<T>& r) {
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<uint4*>(head + d0) = r.u[0];
+        *reinterpret_cast<uint4*>(head + d1) = r.u[1];
+    } else if constexpr (SPLIT_PIECES) {
+        *reinterpret_cast<uint2*>(head + d0) = make_uint2(r.u[0].x, r.u[0].y);
+        *reinterpret_cast<uint2*>(head + d1) = make_uint2(r.u[0].z, r.u[0].w);
+    } else {
+        *reinterpret_cast<uint4*>(head + d0) = r.u[0];
+    }
+}
 
 __device__ __forceinline__ float weight_at(const void* p, int i, int dtype) {
     if (p == nullptr) return 1.f;
@@ -41,103 +72,236 @@ __device__ __forceinline__ float weight_at(const void* p, int i, int dtype) {
     return dtype == DIROTQ_DTYPE_F16 ? __half2float(__ushort_as_half(u)) : __uint_as_float(static_cast<uint32_t>(u) << 16);
 }
 
-template <typename T, int LANES>
-__global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const QkParams p) {
-    constexpr int GROUPS = kThreads / LANES;
-    __shared__ float s_head[GROUPS][LANES * 8];
-    const int sub = threadIdx.x & (LANES - 1), group = threadIdx.x / LANES;
-    const int d0 = sub * 8;
-    const bool has = d0 < p.D;
-    grid_dependency_wait();  // x is the previous kernel's output
-    grid_launch_dependents();
-    const int m = blockIdx.x;
-    const int pos = p.positions != nullptr ? __ldg(p.positions + m) : m;
-    if (p.rope != DIROTQ_ROPE_NONE && (pos < 0 || pos >= p.num_positions)) return;  // padding
-    int slot = m;
-    if (p.slots != nullptr) {
-        slot = __ldg(p.slots + m);
-        if (slot < 0 || slot >= p.num_slots) return;
-    }
-    // the angles of this lane's elements: element d is turned by c[d], s[d] (s with the sign of its place in the pair)
-    float c[8], s[8];
+template <typename T>
+constexpr int kHeads = sizeof(T) == 4 ? 2 : 4;  // sets of heads a warp takes at once
+
+// How the elements of a head lie on its lanes and find their partners.
+enum Style {
+    PLAIN,   // no rotation: element d0 + i of lane sub, d0 = 8 sub
+    PAIRS,   // the same; partners are neighbours
+    SPLIT,   // halves of the whole head: elements 4 sub + i and D/2 + 4 sub + i, i < 4: partners lie in one lane
+    HALVES,  // halves of a part of the head, of any length: as PAIRS, partners through shared memory
+};
+
+// STYLE; LANES: lanes of a head where head_dim is 64, 72 or 128, 0: p.L, any.
+template <typename T, int STYLE, int LANES>
+__global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 2 : 3) qk_norm_rope_kernel(const __grid_constant__ QkParams p) {
+    constexpr int HEADS = kHeads<T>;
+    constexpr int PITCH = 9;  // words of a lane's eight elements in shared memory: odd, so that a warp's reads of one of them fall into 32 banks
+    __shared__ float s_head[STYLE == HALVES ? kThreads / 32 : 1][32 * PITCH];
+    __shared__ __align__(16) float s_w[2][256];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int L = LANES ? LANES : p.L, per_warp = LANES ? 32 / (LANES ? LANES : 1) : p.per_warp;
+    const int sub = lane % L, in_warp = lane / L;  // place in the head, head in the set
+    const int head0 = lane - sub;                  // the lane that holds the head's first elements
+    const bool lives = 32 % (LANES ? LANES : 1) == 0 && LANES ? true : in_warp < per_warp;
     const int half = p.rot >> 1;
-    if (p.rope != DIROTQ_ROPE_NONE) {
-        const float* cs = p.cos_table + static_cast<long long>(pos) * p.ld_table;
-        const float* sn = p.sin_table + static_cast<long long>(pos) * p.ld_table;
+    const int d0 = STYLE == SPLIT ? 4 * sub : 8 * sub, d1 = STYLE == SPLIT ? half + 4 * sub : d0 + 4;  // elements d0 + i, d1 + i, i < 4
+    auto element = [&](int i) { return i < 4 ? d0 + i : d1 + i - 4; };
+    // HALVES: where the partners of this lane's elements will lie; the spare ninth word holds the zero that what is not turned takes instead (an
+    // infinity in some partner's place would leave NaN)
+    float* const s_mine = &s_head[STYLE == HALVES ? warp : 0][lane * PITCH];
+    const float* s_partner[8];
+    if constexpr (STYLE == HALVES) {
+        s_mine[8] = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int d = d0 + i;
-            c[i] = 1.f;
-            s[i] = 0.f;
-            if (d < p.rot) {
-                const int a = p.rope == DIROTQ_ROPE_PAIRS ? d >> 1 : d < half ? d : d - half;
-                const bool second = p.rope == DIROTQ_ROPE_PAIRS ? (d & 1) != 0 : d >= half;
-                c[i] = __ldg(cs + a);
-                s[i] = second ? __ldg(sn + a) : -__ldg(sn + a);
-            }
+            const int d = d0 + i, from = d < half ? d + half : d - half;
+            s_partner[i] = lives && d < p.rot ? &s_head[warp][(head0 + (from >> 3)) * PITCH + (from & 7)] : s_mine + 8;
         }
     }
-    const int heads = p.hq + p.hk + (p.copy_v ? p.hk : 0);
-    const T* row = static_cast<const T*>(p.x) + static_cast<long long>(m) * p.ldx;
-    // (every lane of a warp makes the same number of turns: shuffles below take whole warps)
-    for (int h0 = 0; h0 < heads; h0 += GROUPS) {
-        const int h = h0 + group;
-        const bool live = h < heads && has;
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
-        if (live) load8<T>(row + static_cast<long long>(h) * p.D + d0, v);
-        const bool is_v = h >= p.hq + p.hk;
-        if (p.norm) {
-            float ss = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
-#pragma unroll
-            for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            const float r = rsqrtf(ss * p.inv_dim + p.eps);
-            if (live && !is_v) {
-                const void* w = h < p.hq ? p.qw : p.kw;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= r * weight_at(w, d0 + i, p.wdtype);
-            }
+    const bool weighted = p.qw != nullptr || p.kw != nullptr;
+    grid_dependency_wait();  // x is the previous kernel's output
+    grid_launch_dependents();
+    if (weighted) {
+        for (int i = threadIdx.x; i < p.D; i += kThreads) {
+            s_w[0][i] = weight_at(p.qw, i, p.wdtype);
+            s_w[1][i] = weight_at(p.kw, i, p.wdtype);
         }
-        float o[8];
+        __syncthreads();
+    }
+    for (int item = blockIdx.x * (kThreads / 32) + warp; item < p.items; item += gridDim.x * (kThreads / 32)) {
+        // a turn: one token's q, k or v heads, or a part of them
+        const int m = item / p.parts;
+        int part = item - m * p.parts;
+        const int kind = part < p.parts_q ? 0 : part < p.parts_q + p.parts_k ? 1 : 2;
+        part -= kind == 0 ? 0 : kind == 1 ? p.parts_q : p.parts_q + p.parts_k;
+        const int set = HEADS * per_warp;
+        const int h_end = min(kind == 0 ? p.hq : p.hk, (part + 1) * p.part_sets * set);
+        int h0 = part * p.part_sets * set;
+        const T* from = static_cast<const T*>(p.x) + static_cast<long long>(m) * p.ldx + (kind == 0 ? 0 : kind == 1 ? p.hq : p.hq + p.hk) * p.D;
+        Raw8<T> raw[HEADS];
+        auto load_set = [&]() {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = v[i];
-        if (p.rope == DIROTQ_ROPE_PAIRS) {
-            if (!is_v) {
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    o[i] = v[i] * c[i] + v[i + 1] * s[i];
-                    o[i + 1] = v[i + 1] * c[i + 1] + v[i] * s[i + 1];
-                }
+            for (int j = 0; j < HEADS; ++j) {
+                const int h = h0 + j * per_warp + in_warp;
+                raw[j] = Raw8<T>();
+                if (lives && h < h_end) raw[j] = load_pieces<T, STYLE == SPLIT>(from + h * p.D, d0, d1);
             }
-        } else if (p.rope == DIROTQ_ROPE_HALVES) {
-            __syncwarp();
+        };
+        load_set();
+        const int pos = STYLE != PLAIN && p.positions != nullptr ? __ldg(p.positions + m) : m;
+        const int slot = p.slots != nullptr ? __ldg(p.slots + m) : m;
+        // padding (the same for the whole warp)
+        if (STYLE != PLAIN && (pos < 0 || pos >= p.num_positions)) continue;
+        if (p.slots != nullptr && (slot < 0 || slot >= p.num_slots)) continue;
+        T* out = kind == 0   ? static_cast<T*>(p.q_out) + static_cast<long long>(m) * p.ldq
+                 : kind == 1 ? static_cast<T*>(p.k_out) + static_cast<long long>(slot) * p.ldk
+                             : static_cast<T*>(p.v_out) + static_cast<long long>(slot) * p.ldv;
+        if (kind == 2) {
+            for (;;) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s_head[group][d0 + i] = v[i];
-            __syncwarp();
-            if (!is_v) {
+                for (int j = 0; j < HEADS; ++j) {
+                    const int h = h0 + j * per_warp + in_warp;
+                    if (lives && h < h_end) store_pieces<T, STYLE == SPLIT>(out + h * p.D, d0, d1, raw[j]);
+                }
+                if ((h0 += set) >= h_end) break;
+                load_set();
+            }
+            continue;
+        }
+        // With r = 1 / rms, element d becomes r (h[d] w[d] c + h[partner] w[partner] s), s with the sign of d's place in its pair: the weights go
+        // into the token's cosines (c) and sines (s) once for all its heads.  (Where nothing is turned c = w and s = 0.)
+        float c[8], s[8];
+        {
+            if constexpr (STYLE != PLAIN) {
+                const float* cs = p.cos_table + static_cast<long long>(pos) * p.ld_table;
+                const float* sn = p.sin_table + static_cast<long long>(pos) * p.ld_table;
+                if (p.wide_table && lives && (STYLE == PAIRS || STYLE == SPLIT) && d0 + 8 <= p.rot + (STYLE == SPLIT ? 8 : 0)) {
+                    const int a = STYLE == PAIRS ? d0 >> 1 : d0;
+                    const float4 c0 = __ldg(reinterpret_cast<const float4*>(cs + a)), s0 = __ldg(reinterpret_cast<const float4*>(sn + a));
+                    const float cv[4] = {c0.x, c0.y, c0.z, c0.w}, sv[4] = {s0.x, s0.y, s0.z, s0.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int a0 = STYLE == PAIRS ? 2 * k : k, a1 = STYLE == PAIRS ? 2 * k + 1 : k + 4;
+                        c[a0] = c[a1] = cv[k];
+                        s[a0] = -sv[k];
+                        s[a1] = sv[k];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int d = element(i);
+                        c[i] = 1.f;
+                        s[i] = 0.f;
+                        if (lives && d < p.rot) {
+                            const int a = STYLE == PAIRS ? d >> 1 : d < half ? d : d - half;
+                            const bool second = STYLE == PAIRS ? (d & 1) != 0 : d >= half;
+                            c[i] = __ldg(cs + a);
+                            s[i] = second ? __ldg(sn + a) : -__ldg(sn + a);
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) c[i] = 1.f;
+            }
+            if (weighted && lives) {
+                const float* w = s_w[kind];
+                const float4 w0 = *reinterpret_cast<const float4*>(w + d0), w1 = *reinterpret_cast<const float4*>(w + d1);
+                const float wv[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int d = d0 + i;
-                    if (d < p.rot) o[i] = v[i] * c[i] + s_head[group][d < half ? d + half : d - half] * s[i];
+                    c[i] *= wv[i];
+                    if constexpr (STYLE == PAIRS) s[i] *= wv[i ^ 1];
+                    if constexpr (STYLE == SPLIT) s[i] *= wv[i ^ 4];
+                    if constexpr (STYLE == HALVES) {
+                        const int d = element(i);
+                        s[i] *= w[d >= p.rot ? d : d < half ? d + half : d - half];
+                    }
                 }
             }
         }
-        if (live) {
-            T* out = h < p.hq          ? static_cast<T*>(p.q_out) + static_cast<long long>(m) * p.ldq + h * p.D
-                     : h < p.hq + p.hk ? static_cast<T*>(p.k_out) + static_cast<long long>(slot) * p.ldk + (h - p.hq) * p.D
-                                       : static_cast<T*>(p.v_out) + static_cast<long long>(slot) * p.ldv + (h - p.hq - p.hk) * p.D;
-            store8<T>(out + d0, o);
+        for (;;) {
+#pragma unroll
+        for (int j = 0; j < HEADS; ++j) {
+            if (h0 + j * per_warp >= h_end) break;  // (the same for the whole warp)
+            const int h = h0 + j * per_warp + in_warp;
+            float v[8], o[8];
+            unpack8<T>(raw[j], v);
+            float r = 1.f;
+            if (p.norm) {
+                float ss = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
+                if constexpr (LANES == 8 || LANES == 16) {
+#pragma unroll
+                    for (int f = LANES / 2; f > 0; f >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, f);
+                } else {
+                    // (the first step is the largest power of two below L)
+#pragma unroll
+                    for (int f = LANES ? 8 : p.fold; f > 0; f >>= 1) {
+                        const float other = __shfl_down_sync(0xffffffffu, ss, f);
+                        if (sub + f < L) ss += other;
+                    }
+                    ss = __shfl_sync(0xffffffffu, ss, head0);
+                }
+                r = rsqrtf(ss * p.inv_dim + p.eps);
+            }
+            if constexpr (STYLE == PLAIN) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = r * (v[i] * c[i]);
+            } else {
+                float partner[8];
+                if constexpr (STYLE == PAIRS || STYLE == SPLIT) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) partner[i] = v[STYLE == PAIRS ? i ^ 1 : i ^ 4];
+                    if (STYLE == PAIRS && p.rot != p.D) {  // what has no partner takes nothing of one (an infinity there would leave NaN)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (d0 + i >= p.rot) partner[i] = 0.f;
+                    }
+                } else {
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s_mine[i] = v[i];
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) partner[i] = *s_partner[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = r * fmaf(partner[i], s[i], v[i] * c[i]);
+            }
+            if (lives && h < h_end) store_pieces<T, STYLE == SPLIT>(out + h * p.D, d0, d1, pack8<T>(o));
+        }
+        if ((h0 += set) >= h_end) break;
+        load_set();
         }
     }
 }
 
 template <typename T>
-cudaError_t launch_t(const QkParams& p, int M, cudaStream_t stream) {
-    auto kern = p.D <= 32 ? qk_norm_rope_kernel<T, 4> : p.D <= 64 ? qk_norm_rope_kernel<T, 8> : p.D <= 128 ? qk_norm_rope_kernel<T, 16> : qk_norm_rope_kernel<T, 32>;
-    return launch_kernel(kern, M, kThreads, 0, stream, true, p);
+cudaError_t launch_t(QkParams& p, int M, cudaStream_t stream) {
+    p.L = p.D / 8;
+    p.per_warp = 32 / p.L;
+    p.fold = 0;
+    for (int o = 1; o < p.L; o *= 2) p.fold = o;  // the largest power of two below L
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    // A warp's turn takes all sets of a token's q, k or v where that leaves every SM 32 turns, so that angles and weights are fetched once for
+    // all of them; with fewer tokens one set, so that the call is over sooner.
+    const int per = kHeads<T> * p.per_warp, sets_q = (p.hq + per - 1) / per, sets_k = (p.hk + per - 1) / per;
+    const bool whole = static_cast<long long>(M) * 2 >= 32ll * sm_count(device);
+    p.part_sets = whole ? (sets_q > sets_k ? sets_q : sets_k) : 1;
+    p.parts_q = (sets_q + p.part_sets - 1) / p.part_sets;
+    p.parts_k = (sets_k + p.part_sets - 1) / p.part_sets;
+    p.parts = p.parts_q + (p.copy_v ? 2 : 1) * p.parts_k;
+    const long long items = static_cast<long long>(M) * p.parts;
+    if (items > 0x7fffffffll - (1 << 20)) return cudaErrorInvalidValue;  // (the last turn's number stays below 2^31)
+    p.items = static_cast<int>(items);
+    const long long blocks = (items + kThreads / 32 - 1) / (kThreads / 32), most = 8ll * sm_count(device);
+    auto go = [&](auto kern) { return launch_kernel(kern, static_cast<int>(blocks < most ? blocks : most), kThreads, 0, stream, true, p); };
+#define DIROTQ_QK_STYLE(STYLE)                                            \
+    (p.L == 16  ? go(qk_norm_rope_kernel<T, STYLE, 16>)                   \
+     : p.L == 9 ? go(qk_norm_rope_kernel<T, STYLE, 9>)                    \
+     : p.L == 8 ? go(qk_norm_rope_kernel<T, STYLE, 8>)                    \
+                : go(qk_norm_rope_kernel<T, STYLE, 0>))
+    return p.rope == DIROTQ_ROPE_NONE    ? DIROTQ_QK_STYLE(PLAIN)
+           : p.rope == DIROTQ_ROPE_PAIRS ? DIROTQ_QK_STYLE(PAIRS)
+           : p.rot == p.D                ? DIROTQ_QK_STYLE(SPLIT)
+                                         : DIROTQ_QK_STYLE(HALVES);
+#undef DIROTQ_QK_STYLE
 }
 
 bool bad_float(float v) { return !(v >= 0.f) || v > 3.0e38f; }
@@ -187,9 +351,12 @@ cudaError_t launch_qk_norm_rope(const void* x, int dtype, int M, long long ldx, 
     p.norm = qk.norm; p.rope = qk.rope; p.rot = qk.rot_dim;
     p.eps = qk.eps;
     p.inv_dim = 1.f / static_cast<float>(qk.head_dim);
-    p.wdtype = qk.weight_dtype; p.qw = qk.q_weight; p.kw = qk.k_weight;
+    p.wdtype = qk.weight_dtype;
+    p.qw = qk.norm ? qk.q_weight : nullptr;
+    p.kw = qk.norm ? qk.k_weight : nullptr;
     p.cos_table = qk.cos_table; p.sin_table = qk.sin_table; p.ld_table = qk.ld_table;
     p.num_positions = qk.num_positions;
+    p.wide_table = ((reinterpret_cast<uintptr_t>(qk.cos_table) | reinterpret_cast<uintptr_t>(qk.sin_table)) & 15u) == 0 && qk.ld_table % 4 == 0;
     p.positions = qk.rope != DIROTQ_ROPE_NONE ? qk.positions : nullptr;
     p.slots = slots; p.num_slots = num_slots;
     // v in its own place needs no copy

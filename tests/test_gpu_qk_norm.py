@@ -207,6 +207,24 @@ def test_mxfp4_qkv_padding_tokens(M):
     assert torch.equal(y[pad], z[pad]) and torch.equal(y[:, 384:], z[:, 384:]) and not torch.equal(y[~pad], z[~pad])
 
 
+@pytest.mark.parametrize("M,D", [(5, 64), (5, 128), (40, 64), (200, 64), (200, 128)])
+def test_mxfp4_qkv_bits_do_not_depend_on_the_plan(M, D):
+    s = Setup(M, 4, 1, D, D, "halves", torch.bfloat16, 1)
+    g = torch.Generator().manual_seed(2)
+    x, w = torch.randn((M, 320), generator=g).bfloat16().cuda(), dq.dirotq_mxfp4_quantize((torch.randn((s.width, 320), generator=g) * 0.1).cuda())
+    ws = dq.alloc_mxfp4_workspace(M, 320)
+    outs = []
+    try:
+        for columns in (0, 64, 128, 512):
+            dq.dirotq_set_gemm_tile(columns)
+            outs.append(torch.empty((M, s.width), dtype=torch.bfloat16, device="cuda"))
+            dq.dirotq_mxfp4_qkv(x, w, outs[-1], ws, s.plan)
+    finally:
+        dq.dirotq_set_gemm_tile(0)
+    assert dq.dirotq_workspace_status(ws) == 0
+    assert all(torch.equal(o, outs[0]) for o in outs)
+
+
 def test_mxfp4_qkv_refusals():
     w = dq.dirotq_mxfp4_alloc(768, 64)
     x, y = torch.zeros((8, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((8, 768), dtype=torch.bfloat16, device="cuda")
