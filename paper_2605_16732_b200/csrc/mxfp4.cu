@@ -13,50 +13,70 @@ namespace {
 constexpr int kThreads = 256;
 
 // ------------------------------------------------------------------ quantizer, elements along a row
-// A unit is 256 elements of a row (two scale words).  A warp takes a unit at a time, eight elements per lane: four lanes share a block of
-// 32, so the maximum is two shuffles, a block's codes are four words side by side, a warp's codes 128 bytes.
-constexpr int kUnits = 4;  // units per warp, their loads in flight together
+// A unit is 512 elements of a row (four scale words).  A warp takes UNITS of them, sixteen elements per lane and unit, their loads in flight
+// together: two lanes share a block of 32, so its maximum is one shuffle and a scale word three; codes leave as 8 bytes a lane, 256 a warp.  In
+// 16 bits the instructions bound it, not the memory (eight elements per lane: 34 us for 4608 x 12288 in bf16, 40 in fp32).
+template <typename T>
+struct Raw16 {
+    Raw8<T> h[2];
+};
+// ALIGN: bytes that rows' pieces of 16 elements are aligned to: 32 (in 16 bits one load), 16, or 0 (element by element)
+template <typename T, int ALIGN>
+__device__ __forceinline__ Raw16<T> load_raw16(const T* row, int k0, int K) {
+    Raw16<T> r;
+    if (ALIGN == 32 && sizeof(T) == 2 && k0 + 16 <= K) {
+        uint4 &a = r.h[0].u[0], &b = r.h[1].u[0];
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+                     : "l"(row + k0));
+    } else {
+        r.h[0] = load_raw8<T>(row, k0, K, ALIGN != 0);
+        r.h[1] = load_raw8<T>(row, k0 + 8, K, ALIGN != 0);
+    }
+    return r;
+}
 
-template <typename T, int RULE, bool WIDE>
+template <typename T, int RULE, int ALIGN, int UNITS>
 __global__ void __launch_bounds__(kThreads) mx_quantize_rows_kernel(const T* __restrict__ x, long long ldx, int rows, int K, int nkb, int pitch,
                                                                     uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
     const int lane = threadIdx.x & 31;
-    const unsigned units = static_cast<unsigned>(rows) * nkb;  // (at most 2^31 - 1, see check_shape)
-    const unsigned first = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
+    const int per_row = (nkb + 1) >> 1;
+    const unsigned units = static_cast<unsigned>(rows) * per_row;  // (at most 2^31 - 1, see check_shape)
+    const unsigned first = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * UNITS;
     if (first >= units) return;
-    int row = static_cast<int>(first / nkb), kb = static_cast<int>(first % nkb);
+    int row = static_cast<int>(first / per_row), u = static_cast<int>(first % per_row);
     // the previous kernel of the stream may still read the workspace this one writes, or write x
     grid_dependency_wait();
     grid_launch_dependents();
-    Raw8<T> raw[kUnits];
+    Raw16<T> raw[UNITS];
     {
-        int r = row, b = kb;
+        int r = row, b = u;
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            if (r < rows) raw[u] = load_raw8<T>(x + r * ldx, b * 256 + lane * 8, K, WIDE);
-            if (++b == nkb) { b = 0; ++r; }
+        for (int j = 0; j < UNITS; ++j) {
+            if (r < rows) raw[j] = load_raw16<T, ALIGN>(x + r * ldx, b * 512 + lane * 16, K);
+            if (++b == per_row) { b = 0; ++r; }
         }
     }
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
+    for (int j = 0; j < UNITS; ++j) {
         if (row >= rows) break;  // (the same for the whole warp)
-        float v[8];
-        unpack8<T>(raw[u], v);
-        uint32_t am = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) am = max(am, __float_as_uint(v[i]) & 0x7fffffffu);
+        uint32_t am = max(abs_max_bits<T>(raw[j].h[0]), abs_max_bits<T>(raw[j].h[1]));
         am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
-        am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
-        const int k0 = kb * 256 + lane * 8;
         const uint32_t byte = mx_scale_byte<RULE>(am);
-        const uint32_t word = mx_codes8(v, byte);
-        if (k0 < pitch * 2) *reinterpret_cast<uint32_t*>(codes + static_cast<size_t>(row) * pitch + k0 / 2) = word;
-        // lane 16 h gathers the bytes of blocks 4 h .. 4 h + 3 of the unit
-        uint32_t sw = byte << (8 * ((lane >> 2) & 3));
+        float v[8];
+        unpack8<T>(raw[j].h[0], v);
+        const uint32_t w0 = mx_codes8(v, byte);
+        unpack8<T>(raw[j].h[1], v);
+        const uint32_t w1 = mx_codes8(v, byte);
+        const int at = u * 256 + lane * 8;  // of the row's bytes
+        if (at < pitch) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(row) * pitch + at) = make_uint2(w0, w1);
+        // lane 8 h gathers the bytes of blocks 4 h .. 4 h + 3 of the unit
+        uint32_t sw = byte << (8 * ((lane >> 1) & 3));
+        sw |= __shfl_xor_sync(0xffffffffu, sw, 2);
         sw |= __shfl_xor_sync(0xffffffffu, sw, 4);
-        sw |= __shfl_xor_sync(0xffffffffu, sw, 8);
-        if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(scales + mx_scale_word(row, kb * 2 + (lane >> 4), nkb)) = sw;
-        if (++kb == nkb) { kb = 0; ++row; }
+        const int ak = u * 4 + (lane >> 3);
+        if ((lane & 7) == 0 && ak < 2 * nkb) *reinterpret_cast<uint32_t*>(scales + mx_scale_word(row, ak, nkb)) = sw;
+        if (++u == per_row) { u = 0; ++row; }
     }
 }
 
@@ -124,53 +144,77 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_cols_kernel(const T* __r
 }
 
 // ------------------------------------------------------------------ dequantizer: the quantizer's units, backwards
-template <typename T, bool WIDE>
+template <typename T, int ALIGN>
+__device__ __forceinline__ void store_raw16(T* row, int k0, int K, const Raw16<T>& r) {
+    if (ALIGN == 32 && sizeof(T) == 2 && k0 + 16 <= K) {
+        const uint4 &a = r.h[0].u[0], &b = r.h[1].u[0];
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + k0), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y),
+                     "r"(b.z), "r"(b.w)
+                     : "memory");
+        return;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int k = k0 + 8 * h;
+        if (ALIGN != 0 && k + 8 <= K) {
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) reinterpret_cast<uint4*>(row + k)[i] = r.h[h].u[i];
+        } else {
+            union { Raw8<T> r; T t[8]; } c;
+            c.r = r.h[h];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < K) row[k + i] = c.t[i];
+        }
+    }
+}
+
+template <typename T, int ALIGN, int UNITS>
 __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int K,
                                                                  int nkb, int pitch, T* __restrict__ y, long long ldy) {
     const int lane = threadIdx.x & 31;
-    const unsigned units = static_cast<unsigned>(rows) * nkb;
-    const unsigned first = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits;
+    const int per_row = (nkb + 1) >> 1;
+    const unsigned units = static_cast<unsigned>(rows) * per_row;
+    const unsigned first = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * UNITS;
     if (first >= units) return;
-    int row = static_cast<int>(first / nkb), kb = static_cast<int>(first % nkb);
+    int row = static_cast<int>(first / per_row), u = static_cast<int>(first % per_row);
     grid_dependency_wait();
     grid_launch_dependents();
-    uint32_t word[kUnits], sw[kUnits];
+    uint2 word[UNITS];
+    uint32_t sw[UNITS];
     {
-        int r = row, b = kb;
+        int r = row, b = u;
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            word[u] = sw[u] = 0;
+        for (int j = 0; j < UNITS; ++j) {
+            word[j] = make_uint2(0, 0);
+            sw[j] = 0;
             if (r < rows) {
-                const int k0 = b * 256 + lane * 8;
-                if (k0 < pitch * 2) word[u] = *reinterpret_cast<const uint32_t*>(codes + static_cast<size_t>(r) * pitch + k0 / 2);
-                sw[u] = *reinterpret_cast<const uint32_t*>(scales + mx_scale_word(r, b * 2 + (lane >> 4), nkb));
+                const int at = b * 256 + lane * 8, ak = b * 4 + (lane >> 3);
+                if (at < pitch) word[j] = *reinterpret_cast<const uint2*>(codes + static_cast<size_t>(r) * pitch + at);
+                if (ak < 2 * nkb) sw[j] = *reinterpret_cast<const uint32_t*>(scales + mx_scale_word(r, ak, nkb));
             }
-            if (++b == nkb) { b = 0; ++r; }
+            if (++b == per_row) { b = 0; ++r; }
         }
     }
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
+    for (int j = 0; j < UNITS; ++j) {
         if (row >= rows) break;
-        const int k0 = kb * 256 + lane * 8;
-        const float s = e8m0_value((sw[u] >> (8 * ((lane >> 2) & 3))) & 0xffu);
-        float v[8];
+        const float s = e8m0_value((sw[j] >> (8 * ((lane >> 1) & 3))) & 0xffu);
+        Raw16<T> out;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 p = from_e2m1x2((word[u] >> (8 * i)) & 0xffu);
-            v[2 * i] = p.x * s;
-            v[2 * i + 1] = p.y * s;
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t w = h == 0 ? word[j].x : word[j].y;
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 p = from_e2m1x2((w >> (8 * i)) & 0xffu);
+                v[2 * i] = p.x * s;
+                v[2 * i + 1] = p.y * s;
+            }
+            out.h[h] = pack8<T>(v);
         }
-        T* out = y + row * ldy;
-        if (WIDE && k0 + 8 <= K) {
-            const Raw8<T> r = pack8<T>(v);
-#pragma unroll
-            for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) reinterpret_cast<uint4*>(out + k0)[i] = r.u[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k0 + i < K) out[k0 + i] = from_f32<T>(v[i]);
-        }
-        if (++kb == nkb) { kb = 0; ++row; }
+        store_raw16<T, ALIGN>(y + row * ldy, u * 512 + lane * 16, K, out);
+        if (++u == per_row) { u = 0; ++row; }
     }
 }
 
@@ -214,13 +258,25 @@ __global__ void __launch_bounds__(kThreads) mx_export_kernel(const uint8_t* __re
         out_scales[static_cast<size_t>(row) * nblk + b / 16] = scales[mx_scale_word(row, b >> 6, nkb) + ((b >> 4) & 3)];
 }
 
-inline bool wide_rows(const void* p, long long ld, int dtype) {
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * static_cast<long long>(dtype_size(dtype)) % 16 == 0;
+// What rows at `p`, `ld` elements apart, are aligned to: 32, 16 or 0 (less than 16).
+inline int row_alignment(const void* p, long long ld, size_t element) {
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * static_cast<long long>(element));
+    return (bits & 31u) == 0 ? 32 : (bits & 15u) == 0 ? 16 : 0;
 }
-inline unsigned unit_blocks(int rows, int nkb) {
-    const long long per = (kThreads / 32) * kUnits;
-    return static_cast<unsigned>((static_cast<long long>(rows) * nkb + per - 1) / per);
+// Units of 512 elements per warp: two where that leaves every SM 32 warps, else one, so that a short call is spread out (256 x 1152 1.7
+// against 2.3 us).
+inline int units_per_warp(const dirotq_mxfp4* t) {
+    return static_cast<long long>(t->rows) * ((t->lay.nkb + 1) / 2) >= 64ll * sm_count(t->device) ? 2 : 1;
 }
+inline int unit_blocks(const dirotq_mxfp4* t, int per_warp) {
+    const long long per = (kThreads / 32) * per_warp;
+    return static_cast<int>((static_cast<long long>(t->rows) * ((t->lay.nkb + 1) / 2) + per - 1) / per);
+}
+// go(kernel of that alignment, units per warp)
+#define DIROTQ_MX_UNITS(KERNEL, ...)                                                                                             \
+    (align == 32   ? (per_warp == 2 ? go(KERNEL<__VA_ARGS__, 32, 2>) : go(KERNEL<__VA_ARGS__, 32, 1>)) \
+     : align == 16 ? (per_warp == 2 ? go(KERNEL<__VA_ARGS__, 16, 2>) : go(KERNEL<__VA_ARGS__, 16, 1>)) \
+                   : (per_warp == 2 ? go(KERNEL<__VA_ARGS__, 0, 2>) : go(KERNEL<__VA_ARGS__, 0, 1>)))
 inline bool fits_grid(long long blocks) { return blocks <= 0x7fffffffll; }
 
 template <typename T>
@@ -229,12 +285,13 @@ cudaError_t quantize_t(const void* x, int layout, long long ldx, int rule, const
     uint8_t* codes = reinterpret_cast<uint8_t*>(t->buffer);
     uint8_t* scales = codes + t->lay.off_scales;
     const bool floor = rule == DIROTQ_MX_SCALE_FLOOR;
-    const bool wide = wide_rows(x, ldx, sizeof(T) == 4 ? DIROTQ_DTYPE_F32 : DIROTQ_DTYPE_BF16);
-    auto rows_kern = wide ? (floor ? mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_FLOOR, true> : mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_CEIL, true>)
-                          : (floor ? mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_FLOOR, false> : mx_quantize_rows_kernel<T, DIROTQ_MX_SCALE_CEIL, false>);
-    if (layout == DIROTQ_LAYOUT_NK)
-        return launch_kernel(rows_kern, static_cast<int>(unit_blocks(t->rows, t->lay.nkb)), kThreads, 0, stream, true, in, ldx, t->rows, t->K, t->lay.nkb,
-                             t->lay.pitch, codes, scales);
+    if (layout == DIROTQ_LAYOUT_NK) {
+        const int align = row_alignment(x, ldx, sizeof(T)), per_warp = units_per_warp(t);
+        auto go = [&](auto kern) {
+            return launch_kernel(kern, unit_blocks(t, per_warp), kThreads, 0, stream, true, in, ldx, t->rows, t->K, t->lay.nkb, t->lay.pitch, codes, scales);
+        };
+        return floor ? DIROTQ_MX_UNITS(mx_quantize_rows_kernel, T, DIROTQ_MX_SCALE_FLOOR) : DIROTQ_MX_UNITS(mx_quantize_rows_kernel, T, DIROTQ_MX_SCALE_CEIL);
+    }
     auto kern = floor ? mx_quantize_cols_kernel<T, DIROTQ_MX_SCALE_FLOOR, 1> : mx_quantize_cols_kernel<T, DIROTQ_MX_SCALE_CEIL, 1>;
     int width = 32;
     if constexpr (sizeof(T) == 2) {
@@ -416,17 +473,18 @@ dirotq_status_t dirotq_mxfp4_dequantize(const dirotq_mxfp4_t* t, void* y, int y_
     if (st != DIROTQ_OK) return st;
     const uint8_t* codes = reinterpret_cast<const uint8_t*>(t->buffer);
     const uint8_t* scales = codes + t->lay.off_scales;
-    const bool wide = wide_rows(y, ldy, y_dtype);
-    const int blocks = static_cast<int>(unit_blocks(t->rows, t->lay.nkb));
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    auto go = [&](auto* out) {
+    const int align = row_alignment(y, ldy, dtype_size(y_dtype)), per_warp = units_per_warp(t);
+    auto of_type = [&](auto* out) {
         using T = std::remove_pointer_t<decltype(out)>;
-        return launch_kernel(wide ? mx_dequantize_kernel<T, true> : mx_dequantize_kernel<T, false>, blocks, kThreads, 0, s, true, codes, scales, t->rows,
-                             t->K, t->lay.nkb, t->lay.pitch, out, ldy);
+        auto go = [&](auto kern) {
+            return launch_kernel(kern, unit_blocks(t, per_warp), kThreads, 0, static_cast<cudaStream_t>(stream), true, codes, scales, t->rows, t->K, t->lay.nkb,
+                                 t->lay.pitch, out, ldy);
+        };
+        return DIROTQ_MX_UNITS(mx_dequantize_kernel, T);
     };
-    return done("dirotq_mxfp4_dequantize", y_dtype == DIROTQ_DTYPE_F32    ? go(static_cast<float*>(y))
-                                           : y_dtype == DIROTQ_DTYPE_BF16 ? go(static_cast<__nv_bfloat16*>(y))
-                                                                          : go(static_cast<__half*>(y)));
+    return done("dirotq_mxfp4_dequantize", y_dtype == DIROTQ_DTYPE_F32    ? of_type(static_cast<float*>(y))
+                                           : y_dtype == DIROTQ_DTYPE_BF16 ? of_type(static_cast<__nv_bfloat16*>(y))
+                                                                          : of_type(static_cast<__half*>(y)));
 }
 
 dirotq_status_t dirotq_mxfp4_import(const uint8_t* codes, const uint8_t* scales, const dirotq_mxfp4_t* out, dirotq_stream_t stream) {

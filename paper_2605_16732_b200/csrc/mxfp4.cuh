@@ -5,6 +5,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 namespace dirotq {
 
 // Buffer of an operand [rows, K]:
@@ -168,6 +170,24 @@ __device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = to_f32<T>(c.t[i]);
 }
+// Bits of the largest magnitude (as fp32) among eight elements as they lie in memory.  In 16 bits the maximum is taken on pairs of patterns without
+// their signs, whose order is that of the magnitudes (infinity above every number, NaN above that).
+template <typename T>
+__device__ __forceinline__ uint32_t abs_max_bits(const Raw8<T>& r) {
+    if constexpr (sizeof(T) == 4) {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
+        return m;
+    } else {
+        const uint32_t m = __vmaxu2(__vmaxu2(r.u[0].x & 0x7fff7fffu, r.u[0].y & 0x7fff7fffu), __vmaxu2(r.u[0].z & 0x7fff7fffu, r.u[0].w & 0x7fff7fffu));
+        const uint32_t top = max(m & 0xffffu, m >> 16);
+        if constexpr (std::is_same_v<T, __nv_bfloat16>) return top << 16;
+        else return __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(top))));
+    }
+}
+
 // Elements k0 .. k0 + 7 of a row of K as they are, zeros behind K.  (Not converted here: a conversion would wait for the load, and several are to be
 // in flight.)
 template <typename T>

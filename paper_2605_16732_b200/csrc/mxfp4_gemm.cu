@@ -314,9 +314,7 @@ __device__ __forceinline__ void quantize_resident(const MxKernelParams& p, uint3
         for (int j = 0; j < AHEAD; ++j) {
             float v[8];
             unpack8<T>(raw[j], v);
-            uint32_t am = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) am = max(am, __float_as_uint(v[i]) & 0x7fffffffu);
+            uint32_t am = abs_max_bits<T>(raw[j]);
             am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
             am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
             const uint32_t byte = p.scale_rule == DIROTQ_MX_SCALE_FLOOR ? mx_scale_byte<DIROTQ_MX_SCALE_FLOOR>(am) : mx_scale_byte<DIROTQ_MX_SCALE_CEIL>(am);
