@@ -10,12 +10,12 @@
 // to the MMA warp through an mbarrier.  An atom's 32-bit words hold the scales of two instructions; the instruction descriptor's scale
 // ids (0 or 2) pick the half.
 //
-// Roles (384 threads): warp 0 TMA producer, warp 1 MMA issuer and owner of the tensor memory, warps 2..3 scale copiers, warps 4..11 epilogue in
-// two warpgroups.  Plans:
+// Roles: warp 0 TMA producer, warp 1 MMA issuer and owner of the tensor memory, warps 2..3 scale copiers, 16 (or 8) epilogue warps in two
+// groups.  Plans:
 //   PAIR: clusters of two CTAs share every MMA (cta_group::2, M = 256): 256 rows x 256 columns per pair; each CTA holds its own 128 rows of
-//         a, half of b's 256 rows, and the scales of both halves.  One 256-column accumulator, a warpgroup per half of it: the epilogue
+//         a, half of b's 256 rows, and the scales of both halves.  One 256-column accumulator, an epilogue group per half of it: the group
 //         reads it into registers and hands it back before it converts.
-//   single CTAs, 128 rows x 128 or 64 columns: two accumulators, the two epilogue warpgroups take tiles in turn.
+//   single CTAs, 128 rows x 128 or 64 columns: two accumulators, the two epilogue groups take tiles in turn.
 //   FUSE (single CTAs, few rows): the activations are quantized by the kernel itself, by every CTA for itself, into shared memory, where
 //         their codes and scales stay; the ring carries b alone.
 // Every plan adds an output element's products in the same order, so that a row's bits do not depend on the plan.
@@ -31,8 +31,9 @@ namespace {
 constexpr int BM = 128;
 constexpr int ATOMS = 1024;            // bytes of the scales of 128 rows and one k-block
 constexpr int A_BYTES = BM * 128;      // 16 KB
-constexpr int NUM_THREADS = 384;
-constexpr int NUM_EPI_WARPS = 8;
+constexpr int EPI_WARPS = 16;
+constexpr int NUM_THREADS = 128 + EPI_WARPS * 32;
+constexpr int GROUP_THREADS = EPI_WARPS * 16;  // of one of the two epilogue groups
 
 template <int BN, bool PAIR, bool FUSE>
 struct MxPlan {
@@ -42,13 +43,14 @@ struct MxPlan {
     static constexpr int SF_OFFSET = A_STAGE + B_BYTES;                       // scales of a (unless they stay), then of b
     static constexpr int SFB_OFFSET = SF_OFFSET + (FUSE ? 0 : ATOMS);
     static constexpr int STAGE_BYTES = SFB_OFFSET + NB * ATOMS;               // pair 35 KB, single 34 / 26 KB, fused 17 / 9 KB
-    static constexpr int STAGES = FUSE ? (BN == 64 ? 10 : 6) : (BN == 64 ? 8 : 6);
-    static constexpr int RESIDENT = FUSE ? (BN == 64 ? 120 : 112) * 1024 : 0; // codes and scales of the activations
+    static constexpr int STAGES = FUSE ? (BN == 64 ? 16 : 8) : (BN == 64 ? 8 : 6);
+    static constexpr int RESIDENT = FUSE ? 64 * 1024 : 0;                     // codes and scales of the activations (see kFuseUnits)
     static constexpr int BAR_OFFSET = RESIDENT + STAGES * STAGE_BYTES;
-    static constexpr int BIAS_OFFSET = BAR_OFFSET + 512;                      // per warpgroup two buffers of 128 values
+    static constexpr int BIAS_OFFSET = BAR_OFFSET + 512;                      // per epilogue group two buffers of 128 values
     static constexpr int HEADW_OFFSET = BIAS_OFFSET + 4 * 128 * 4;            // q and k weights of a head, 128 values each
-    static constexpr int EDGE_OFFSET = HEADW_OFFSET + 2 * 128 * 4;            // 8 rows x 128 bytes per epilogue warp: rows of y of any alignment
-    static constexpr int SMEM_BYTES = EDGE_OFFSET + NUM_EPI_WARPS * 1024 + 1024;
+    static constexpr int EDGE_OFFSET = HEADW_OFFSET + 2 * 128 * 4;            // 8 rows x 64 bytes per epilogue warp: rows of y of any alignment
+    static constexpr int SUM_OFFSET = EDGE_OFFSET + EPI_WARPS * 512;          // sums of squares of 32 rows per epilogue warp
+    static constexpr int SMEM_BYTES = SUM_OFFSET + EPI_WARPS * 128 + 1024;
     static constexpr int ACC_BUFS = PAIR ? 1 : 2;
     static constexpr int TMEM_SF = ACC_BUFS * BN;                             // columns of the scales: per stage 8 for a, 8 per 128 columns
     static constexpr int SF_COLS = 8 * (1 + NB);
@@ -158,19 +160,19 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// Named barrier ID of the 128 threads of an epilogue warpgroup that makes them agree: true if any of them brings true.
-template <int ID>
+// Named barrier ID of the THREADS of an epilogue group that makes them agree: true if any of them brings true.
+template <int ID, int THREADS>
 __device__ __forceinline__ bool group_any(bool mine) {
     uint32_t any;
     asm volatile(
         "{\n\t"
         ".reg .pred pin, pout;\n\t"
         "setp.ne.u32 pin, %1, 0;\n\t"
-        "bar.red.or.pred pout, %2, 128, pin;\n\t"
+        "bar.red.or.pred pout, %2, %3, pin;\n\t"
         "selp.u32 %0, 1, 0, pout;\n\t"
         "}\n"
         : "=r"(any)
-        : "r"(static_cast<uint32_t>(mine)), "n"(ID)
+        : "r"(static_cast<uint32_t>(mine)), "n"(ID), "n"(THREADS)
         : "memory");
     return any != 0;
 }
@@ -207,6 +209,26 @@ __device__ __forceinline__ void transpose4(uint32_t (&w)[4], int t) {
     }
 }
 
+// Run of 32 columns from n0 of eight rows from row0, lane (l / 4, l % 4) with 8 consecutive columns of its row: straight where rows are wide enough
+// apart and whole, else through 512 bytes of shared memory and written by consecutive lanes.
+__device__ __forceinline__ void store_run(const MxKernelParams& p, int row0, int rows, int n0, int lane, const uint4& out, uint32_t edge, bool whole) {
+    uint16_t* y = reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row0) * p.ldy + n0;
+    const int t = lane & 3, r4 = lane >> 2;
+    if (whole) {
+        if (r4 < rows) __stcs(reinterpret_cast<uint4*>(y + r4 * p.ldy + 8 * t), out);
+        return;
+    }
+    __syncwarp();
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(edge + r4 * 64 + t * 16), "r"(out.x), "r"(out.y), "r"(out.z), "r"(out.w) : "memory");
+    __syncwarp();
+#pragma unroll 1
+    for (int r = 0; r < rows; ++r) {
+        uint16_t e;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(e) : "r"(edge + r * 64 + 2 * lane) : "memory");
+        if (n0 + lane < p.N) y[r * p.ldy + lane] = e;
+    }
+}
+
 // Cosines and sines of four consecutive angles (`wide`: 16-byte aligned).
 __device__ __forceinline__ void load_angles(const float* cs, const float* sn, int wide, float (&c)[4], float (&s)[4]) {
     if (wide) {
@@ -222,68 +244,124 @@ __device__ __forceinline__ void load_angles(const float* cs, const float* sn, in
     }
 }
 
-// Norm and rotation of one head of a row, held by four lanes: lane t has elements 32 m + 8 t + e of its R * 32.  `turned`: false for rows that keep
-// what the projection made them (all lanes take part in the sum).
-template <int R>
-__device__ __forceinline__ void head_norm_rope(float (*v)[8], bool turned, const float* w, int t, int pos, const MxKernelParams& p) {
-    if (p.norm) {
-        float s0 = 0.f, s1 = 0.f;
+// The columns of a fused projection's tile that one warp has: two runs of 32 columns, at `run0` and `run1` of the group's, of SETS * 16 rows from
+// row0.  Runs are halves of one head: of 64 columns (run1 = run0 + 32), or of 128, whose other halves are another warp's (run1 = run0 + 64: element
+// i and i + D/2 are always in one warp); those two warps add up their sums of squares through s_sum, `pair_bar` their named barrier.
+//
+// raw[set][run][4 k + 2 hi + e] is column 8 k + 2 t + e of row 16 set + 8 hi + l / 4 as it is loaded, and, exchanged within the row's four lanes,
+// column 8 t + 2 k + e.
+template <int SETS, bool F16>
+__device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], const MxKernelParams& p, int row0, int n0, int run0, int run1, int lane, const float* s_b,
+                                            const float* s_hw, float* s_sum, const float* s_sum_other, int pair_bar, uint32_t edge, bool whole) {
+    const int t = lane & 3, r4 = lane >> 2;
+    const bool head = n0 + run0 < p.k_end;  // q or k (the same for the whole warp, and for the two of a head)
+    float ss[SETS][2];
 #pragma unroll
-        for (int m = 0; m < R; ++m)
+    for (int set = 0; set < SETS; ++set)
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                s0 = fmaf(v[m][e], v[m][e], s0);
-                s1 = fmaf(v[m][e + 1], v[m][e + 1], s1);
-            }
-        s0 += s1;
-        s0 += __shfl_xor_sync(0xffffffffu, s0, 1);
-        s0 += __shfl_xor_sync(0xffffffffu, s0, 2);
-        if (!turned) return;
-        const float r = rsqrtf(s0 * p.inv_dim + p.eps);
+        for (int hi = 0; hi < 2; ++hi) {
+            float sum = 0.f;
 #pragma unroll
-        for (int m = 0; m < R; ++m)
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                const float4 g = *reinterpret_cast<const float4*>(w + 32 * m + 8 * t + e);
-                v[m][e] *= r * g.x;
-                v[m][e + 1] *= r * g.y;
-                v[m][e + 2] *= r * g.z;
-                v[m][e + 3] *= r * g.w;
-            }
-    }
-    if (!turned) return;
-    const float* cs = p.cos_table + static_cast<long long>(pos) * p.ld_table;
-    const float* sn = p.sin_table + static_cast<long long>(pos) * p.ld_table;
-    if (p.rope == DIROTQ_ROPE_PAIRS) {  // angles 16 m + 4 t ..
-#pragma unroll
-        for (int m = 0; m < R; ++m) {
-            float c[4], s[4];
-            load_angles(cs + 16 * m + 4 * t, sn + 16 * m + 4 * t, p.wide_table, c, s);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float a = v[m][2 * k], b = v[m][2 * k + 1];
-                v[m][2 * k] = a * c[k] - b * s[k];
-                v[m][2 * k + 1] = a * s[k] + b * c[k];
-            }
-        }
-    } else if (p.rope == DIROTQ_ROPE_HALVES) {  // element i and i + R * 16: the same lane, R / 2 runs further on
-#pragma unroll
-        for (int m = 0; m < R / 2; ++m)
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                float c[4], s[4];
-                load_angles(cs + 32 * m + 8 * t + e, sn + 32 * m + 8 * t + e, p.wide_table, c, s);
+            for (int j = 0; j < 2; ++j) {
+                uint32_t even[4], odd[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float a = v[m][e + k], b = v[m + R / 2][e + k];
-                    v[m][e + k] = a * c[k] - b * s[k];
-                    v[m + R / 2][e + k] = a * s[k] + b * c[k];
+                    even[k] = raw[set][j][4 * k + 2 * hi];
+                    odd[k] = raw[set][j][4 * k + 2 * hi + 1];
+                }
+                transpose4(even, t);
+                transpose4(odd, t);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 b = *reinterpret_cast<const float2*>(s_b + (j ? run1 : run0) + 8 * t + 2 * k);
+                    const float x = __uint_as_float(even[k]) + b.x, y = __uint_as_float(odd[k]) + b.y;
+                    sum = fmaf(x, x, fmaf(y, y, sum));
+                    raw[set][j][4 * k + 2 * hi] = __float_as_uint(x);
+                    raw[set][j][4 * k + 2 * hi + 1] = __float_as_uint(y);
                 }
             }
+            ss[set][hi] = sum;
+        }
+    if (head && p.norm) {
+#pragma unroll
+        for (int set = 0; set < SETS; ++set)
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+                ss[set][hi] += __shfl_xor_sync(0xffffffffu, ss[set][hi], 1);
+                ss[set][hi] += __shfl_xor_sync(0xffffffffu, ss[set][hi], 2);
+                if (run1 != run0 + 32 && t == 0) s_sum[16 * set + 8 * hi + r4] = ss[set][hi];
+            }
+        if (run1 != run0 + 32) {
+            asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+#pragma unroll
+            for (int set = 0; set < SETS; ++set)
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) ss[set][hi] += s_sum_other[16 * set + 8 * hi + r4];
+        }
     }
+    const float* w = s_hw + (n0 + run0 < p.q_cols ? 0 : 128);
+    const int at0 = run0 & ((1 << p.head_shift) - 1), at1 = run1 & ((1 << p.head_shift) - 1);  // the runs' places in the head
+#pragma unroll
+    for (int set = 0; set < SETS; ++set)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+            const int row = row0 + 16 * set + 8 * hi + r4;
+            int pos = row;
+            if (head && p.positions != nullptr && row < p.M) pos = __ldg(p.positions + row);
+            if (head && row < p.M && (p.rope == DIROTQ_ROPE_NONE || (pos >= 0 && pos < p.num_positions))) {
+                auto v = [&](int j, int e) -> uint32_t& { return raw[set][j][4 * (e >> 1) + 2 * hi + (e & 1)]; };
+                if (p.norm) {
+                    const float r = rsqrtf(ss[set][hi] * p.inv_dim + p.eps);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int e = 0; e < 8; e += 4) {
+                            const float4 g = *reinterpret_cast<const float4*>(w + (j ? at1 : at0) + 8 * t + e);
+                            v(j, e) = __float_as_uint(__uint_as_float(v(j, e)) * (r * g.x));
+                            v(j, e + 1) = __float_as_uint(__uint_as_float(v(j, e + 1)) * (r * g.y));
+                            v(j, e + 2) = __float_as_uint(__uint_as_float(v(j, e + 2)) * (r * g.z));
+                            v(j, e + 3) = __float_as_uint(__uint_as_float(v(j, e + 3)) * (r * g.w));
+                        }
+                }
+                const long long table = static_cast<long long>(pos) * p.ld_table;
+                auto turn = [&](uint32_t& x, uint32_t& y, float c, float s) {
+                    const float a = __uint_as_float(x), b = __uint_as_float(y);
+                    x = __float_as_uint(a * c - b * s);
+                    y = __float_as_uint(a * s + b * c);
+                };
+                if (p.rope == DIROTQ_ROPE_PAIRS) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float c[4], s[4];
+                        const int a = ((j ? at1 : at0) >> 1) + 4 * t;
+                        load_angles(p.cos_table + table + a, p.sin_table + table + a, p.wide_table, c, s);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) turn(v(j, 2 * k), v(j, 2 * k + 1), c[k], s[k]);
+                    }
+                } else if (p.rope == DIROTQ_ROPE_HALVES) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 4) {
+                        float c[4], s[4];
+                        const int a = at0 + 8 * t + e;
+                        load_angles(p.cos_table + table + a, p.sin_table + table + a, p.wide_table, c, s);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) turn(v(0, e + k), v(1, e + k), c[k], s[k]);
+                    }
+                }
+            }
+            const int rows = min(8, p.M - row0 - 16 * set - 8 * hi);  // (none or less where the tile ends before)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t o[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    o[k] = pack2<F16>(__uint_as_float(raw[set][j][4 * k + 2 * hi]), __uint_as_float(raw[set][j][4 * k + 2 * hi + 1]));
+                store_run(p, row - r4, rows, n0 + (j ? run1 : run0), lane, make_uint4(o[0], o[1], o[2], o[3]), edge, whole);
+            }
+        }
 }
 
-// Quantizes all M rows into shared memory (256 threads): codes at `codes` + (kb groups + row / 8) KB in the layout of a TMA load with the 128-byte
+// Quantizes all M rows into shared memory (the epilogue's warps): codes at `codes` + (kb groups + row / 8) KB in the layout of a TMA load with the 128-byte
 // swizzle, scales at `scales` + kb KB as two atoms.  The arithmetic of mx_quantize_rows_kernel.
 template <typename T>
 __device__ __forceinline__ void quantize_resident(const MxKernelParams& p, uint32_t codes, uint32_t scales, int warp, int lane) {
@@ -291,9 +369,9 @@ __device__ __forceinline__ void quantize_resident(const MxKernelParams& p, uint3
     const T* x = static_cast<const T*>(p.x);
     const int units = p.M * p.nkb;
     int row = warp / p.nkb, kb = warp - row * p.nkb;
-    const int rows_on = NUM_EPI_WARPS / p.nkb, kb_on = NUM_EPI_WARPS - rows_on * p.nkb;
+    const int rows_on = EPI_WARPS / p.nkb, kb_on = EPI_WARPS - rows_on * p.nkb;
 #pragma unroll 1
-    for (int u0 = warp; u0 < units; u0 += AHEAD * NUM_EPI_WARPS) {
+    for (int u0 = warp; u0 < units; u0 += AHEAD * EPI_WARPS) {
         Raw8<T> raw[AHEAD];
         int rows[AHEAD], kbs[AHEAD];
 #pragma unroll
@@ -339,7 +417,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
 mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ MxKernelParams p) {
     using P = MxPlan<BN, PAIR, FUSE>;
     constexpr int NB = P::NB, STAGES = P::STAGES, ACC_BUFS = P::ACC_BUFS, STAGE_BYTES = P::STAGE_BYTES;
-    constexpr int CW = PAIR ? 128 : BN;  // columns of an epilogue warpgroup
+    constexpr int CW = PAIR ? 128 : BN;  // columns of an epilogue group
     constexpr bool SPLIT_REGS = QKV || CW == 128;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -375,9 +453,9 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(tfull_bar(a), 1);
-            mbar_init(tempty_bar(a), PAIR ? 2 * NUM_EPI_WARPS * 32 : NUM_EPI_WARPS * 32 / 2);
+            mbar_init(tempty_bar(a), PAIR ? 4 * GROUP_THREADS : GROUP_THREADS);
         }
-        mbar_init(xready_bar, NUM_EPI_WARPS * 32);
+        mbar_init(xready_bar, EPI_WARPS * 32);
         mbar_init(drain_bar, 1);
         *abort_flag = 0;
         fence_mbar_init();
@@ -402,9 +480,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
     // kernel before they do)
 
     if (warp < 4) {
-        // An epilogue thread holds 32 values in transit beside the 128 it has read: 72 and 208 registers a thread (128 * 72 + 256 * 208 of the
-        // 384 * 168 at launch)
-        if constexpr (SPLIT_REGS) reg_dealloc<72>();
+        if constexpr (SPLIT_REGS) reg_dealloc<56>();  // 128 * 56 + 512 * 104 registers of the 640 * 96 at launch
         if (warp == 0) {
             // ------------------------------------------------------------ producer
             RingPos<STAGES> at;
@@ -532,17 +608,19 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
         }
     } else {
         // ------------------------------------------------------------ epilogue
-        // warp % 4 selects the quadrant of tensor-memory lanes (32 rows); a warpgroup has CW columns: half of a pair's tile, or the whole of every
-        // second tile.  A warp reads its 32 x CW values and hands the accumulator back before it converts them.
+        // Two groups of eight warps; a group has CW columns: half of a pair's tile, or the whole of every second tile.  warp % 4 is the quadrant of
+        // tensor-memory lanes (32 rows) that a warp may read; the two warps of a group and quadrant take 16 rows each, or, where 128 columns are
+        // heads, 64 columns each (store_heads).  A warp reads its values before it hands the accumulator back and converts.
         //
-        // Loads of 16 lanes x 256 bits leave lane l with columns 8 J + 2 t, + 1 (t = l % 4) of rows l / 4 + 8 i (i = 0..3): exchanged within the four
-        // lanes of a row (transpose4), each lane has runs of 8 consecutive columns, 32 m + 8 t, of its four rows, 64 bytes of a row side by side
-        // in a store.  (Through shared memory and TMA stores instead: the same time at K = 12288, and 32 KB that hold a stage of operands
-        // here.)
-        if constexpr (SPLIT_REGS) reg_alloc<208>();
+        // Loads of 16 lanes x 256 bits leave lane l with columns 8 J + 2 t, + 1 (t = l % 4) of rows l / 4 and l / 4 + 8: exchanged within the four lanes
+        // of a row (transpose4), each lane has runs of 8 consecutive columns, 32 m + 8 t, of its two rows, 64 bytes of a row side by side in a
+        // store.  (Through shared memory and TMA stores instead: the same time at K = 12288, and 32 KB that hold a stage of operands here.)
+        if constexpr (SPLIT_REGS) reg_alloc<104>();
         constexpr int RUNS = CW / 32, CH = CW / 64;
-        const int q = warp & 3, group = (warp - 4) >> 2, gt = threadIdx.x & 127;
-        const int t = lane & 3, r4 = lane >> 2;
+        const int q = warp & 3, second = ((warp - 4) >> 2) & 1, group = (warp - 4) >> 3, gt = threadIdx.x - 128 - group * GROUP_THREADS;
+        constexpr bool HEADS128 = QKV && CW == 128;  // the second warp of a quadrant takes other columns, not rows
+        const int first_row = q * 32 + (HEADS128 ? 0 : second * 16);
+        [[maybe_unused]] const int t = lane & 3, r4 = lane >> 2;
         grid_dependency_wait();
         grid_launch_dependents();  // the next kernel may be scheduled as this grid's CTAs leave (it waits for this whole grid)
         if constexpr (FUSE) {
@@ -554,152 +632,87 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             mbar_arrive(xready_bar);
         }
         float* s_hw = reinterpret_cast<float*>(smem_gen + P::HEADW_OFFSET);
-        if constexpr (QKV) {  // (both warpgroups write the same values; each reads behind its own barrier below)
-            const int i = gt & ((1 << p.head_shift) - 1);
-            s_hw[gt] = load_weight(p.qw, i, p.wdtype);
-            s_hw[128 + gt] = load_weight(p.kw, i, p.wdtype);
+        if constexpr (QKV) {  // (both groups write the same values; each reads behind its own barrier below)
+            s_hw[gt] = load_weight(gt < 128 ? p.qw : p.kw, gt & ((1 << p.head_shift) - 1), p.wdtype);
         }
         uint32_t tcount = PAIR ? 0 : group;
         for (int tile = tile_first + (PAIR ? 0 : group * tile_step); tile < num_tiles; tile += PAIR ? tile_step : 2 * tile_step, tcount += PAIR ? 1 : 2) {
-            const int row0 = (tile % num_m_blocks) * TILE_ROWS + (PAIR ? static_cast<int>(cta_rank) * BM : 0) + q * 32;
+            const int row0 = (tile % num_m_blocks) * TILE_ROWS + (PAIR ? static_cast<int>(cta_rank) * BM : 0) + first_row;
             const int n0 = (tile / num_m_blocks) * BN + (PAIR ? group * 128 : 0);
             const uint32_t acc = tcount % ACC_BUFS, use = tcount / ACC_BUFS;
             // the bias of these columns goes to shared memory while the tile's MMAs run (two buffers: a warp can be a tile ahead); the
-            // barrier orders the stores before the reads and makes the warpgroup agree on whether to go on
+            // barrier orders the stores before the reads and makes the group agree on whether to go on
             float* s_b = reinterpret_cast<float*>(smem_gen + P::BIAS_OFFSET) + (group * 2 + (use & 1)) * 128;
             if (gt < CW) s_b[gt] = p.bias != nullptr && n0 + gt < p.N ? load_16(p.bias, n0 + gt, F16) : 0.f;
             const bool failed = !mbar_wait(tfull_bar(acc), use & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
-            if (group == 0 ? group_any<1>(failed) : group_any<2>(failed)) break;
+            if (group == 0 ? group_any<1, GROUP_THREADS>(failed) : group_any<2, GROUP_THREADS>(failed)) break;
             tc_fence_after_sync();
-            const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * BN + (PAIR ? group * 128 : 0);
-            uint32_t raw[2][CH][32];  // [rows 16 h ..][columns 64 c ..][4 j + 2 (row + 8) + (column + 1)], J = 8 c + j
-            const bool stored = row0 < p.M && n0 < p.N;  // (uniform in the warp)
-            if (stored) {
+            const uint32_t taddr = tmem_base + (static_cast<uint32_t>(first_row) << 16) + acc * BN + (PAIR ? group * 128 : 0);
+            const bool stored = row0 < p.M && n0 < p.N;  // (uniform in the warp, and the same in the two of a quadrant that share heads)
+            const bool whole = p.wide_out && n0 + CW <= p.N;
+            const uint32_t edge = smem_base + P::EDGE_OFFSET + static_cast<uint32_t>(warp - 4) * 512u;
+            auto hand_back = [&]() {
+                tc_fence_before_sync();
+                if constexpr (PAIR) mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));  // the leader's barrier
+                else mbar_arrive(tempty_bar(acc));
+            };
+            if constexpr (QKV) {
+                constexpr int SETS = HEADS128 ? 2 : 1;
+                const bool split = HEADS128 && p.head_shift == 7;
+                const int run0 = HEADS128 ? (split ? 32 : 64) * second : 0, run1 = run0 + (split ? 64 : 32);
+                uint32_t raw[SETS][2][16];
+                if (stored) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                    for (int s = 0; s < SETS; ++s) {
+                        tmem_ld_16x256b_x4(taddr + (static_cast<uint32_t>(16 * s) << 16) + run0, raw[s][0]);
+                        tmem_ld_16x256b_x4(taddr + (static_cast<uint32_t>(16 * s) << 16) + run1, raw[s][1]);
+                    }
+                    tmem_ld_wait();
 #pragma unroll
-                    for (int c = 0; c < CH; ++c) tmem_ld_16x256b_x8(taddr + (static_cast<uint32_t>(16 * h) << 16) + c * 64, raw[h][c]);
-                tmem_ld_wait();
+                    for (int s = 0; s < SETS; ++s) {
+                        tmem_ld_fence(raw[s][0]);
+                        tmem_ld_fence(raw[s][1]);
+                    }
+                }
+                hand_back();
+                if (!stored) continue;
+                float* sums = reinterpret_cast<float*>(smem_gen + P::SUM_OFFSET);
+                store_heads<SETS, F16>(raw, p, row0, n0, run0, run1, lane, s_b, s_hw, sums + (warp - 4) * 32, sums + ((warp - 4) ^ 4) * 32,
+                                       3 + group * 4 + q, edge, whole);
+            } else {
+                uint32_t raw[CH][32];  // [columns 64 c ..][4 j + 2 (row + 8) + (column + 1)], J = 8 c + j
+                if (stored) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                    for (int c = 0; c < CH; ++c) tmem_ld_16x256b_x8(taddr + c * 64, raw[c]);
+                    tmem_ld_wait();
 #pragma unroll
-                    for (int c = 0; c < CH; ++c) tmem_ld_fence(raw[h][c]);
-            }
-            tc_fence_before_sync();
-            if constexpr (PAIR) mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));  // the leader's barrier
-            else mbar_arrive(tempty_bar(acc));
-            if (!stored) continue;
-
-            // the rows l / 4 + 8 i of the tile's columns, i = 2 h + hi (of registers that hold h in place 0), rounded and exchanged
-            auto convert = [&](const uint32_t (&src)[CH][32], int hi, uint4 (&out)[RUNS]) {
-#pragma unroll
-                for (int m = 0; m < RUNS; ++m) {
+                    for (int c = 0; c < CH; ++c) tmem_ld_fence(raw[c]);
+                }
+                hand_back();
+                if (!stored) continue;
+                auto convert = [&](int hi, int m) {  // run m of rows l / 4 + 8 hi, rounded and exchanged
                     uint32_t w[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const float2 b = *reinterpret_cast<const float2*>(s_b + 32 * m + 8 * k + 2 * t);
-                        w[k] = pack2<F16>(__uint_as_float(src[m >> 1][16 * (m & 1) + 4 * k + 2 * hi]) + b.x,
-                                          __uint_as_float(src[m >> 1][16 * (m & 1) + 4 * k + 2 * hi + 1]) + b.y);
+                        w[k] = pack2<F16>(__uint_as_float(raw[m >> 1][16 * (m & 1) + 4 * k + 2 * hi]) + b.x,
+                                          __uint_as_float(raw[m >> 1][16 * (m & 1) + 4 * k + 2 * hi + 1]) + b.y);
                     }
                     transpose4(w, t);
-                    out[m] = make_uint4(w[0], w[1], w[2], w[3]);
+                    return make_uint4(w[0], w[1], w[2], w[3]);
+                };
+                if (whole && row0 + 16 <= p.M) {
+                    uint16_t* y = reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row0 + r4) * p.ldy + n0 + 8 * t;
+#pragma unroll
+                    for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+                        for (int m = 0; m < RUNS; ++m) __stcs(reinterpret_cast<uint4*>(y + 8 * hi * p.ldy + 32 * m), convert(hi, m));
+                } else {
+#pragma unroll
+                    for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+                        for (int m = 0; m < RUNS; ++m) store_run(p, row0 + 8 * hi, min(8, p.M - row0 - 8 * hi), n0 + 32 * m, lane, convert(hi, m), edge, whole);
                 }
-            };
-            uint16_t* ytile = reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row0) * p.ldy + n0;
-            const bool whole = p.wide_out && n0 + CW <= p.N;
-            if (!QKV && whole && row0 + 32 <= p.M) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint4 out[RUNS];
-                    convert(raw[i >> 1], i & 1, out);
-                    uint16_t* yrow = ytile + (8 * i + r4) * p.ldy + 8 * t;
-#pragma unroll
-                    for (int m = 0; m < RUNS; ++m) __stcs(reinterpret_cast<uint4*>(yrow + 32 * m), out[m]);
-                }
-                continue;
-            }
-            // Heads, ragged and unaligned tiles.  The loop over the 16-row halves is kept rolled (the second half's registers move into the first's
-            // place): unrolled, its code is fetched for longer than it runs in short calls (64 tokens of q/k/v 14.5 against 13.1 us, 4608
-            // tokens 90 against 84).
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int hi = 0; hi < 2; ++hi) {
-                    const int first = 16 * h + 8 * hi;  // of the eight rows
-                    if (row0 + first >= p.M) continue;
-                    const int row = row0 + first + r4;
-                    uint4 out[RUNS];
-                    if (QKV && n0 < p.k_end) {
-                        float v[RUNS][8];  // columns 32 m + 8 t + e
-#pragma unroll
-                        for (int m = 0; m < RUNS; ++m) {
-                            uint32_t even[4], odd[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                even[k] = raw[0][m >> 1][16 * (m & 1) + 4 * k + 2 * hi];
-                                odd[k] = raw[0][m >> 1][16 * (m & 1) + 4 * k + 2 * hi + 1];
-                            }
-                            transpose4(even, t);
-                            transpose4(odd, t);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const float2 b = *reinterpret_cast<const float2*>(s_b + 32 * m + 8 * t + 2 * k);
-                                v[m][2 * k] = __uint_as_float(even[k]) + b.x;
-                                v[m][2 * k + 1] = __uint_as_float(odd[k]) + b.y;
-                            }
-                        }
-                        int pos = row;
-                        if (p.positions != nullptr && row < p.M) pos = __ldg(p.positions + row);
-                        const bool turned = row < p.M && (p.rope == DIROTQ_ROPE_NONE || (pos >= 0 && pos < p.num_positions));
-                        if (!turned) pos = 0;
-                        if (RUNS == 4 && p.head_shift == 7) {
-                            head_norm_rope<RUNS>(v, turned, s_hw + (n0 < p.q_cols ? 0 : 128), t, pos, p);
-                        } else {
-#pragma unroll
-                            for (int m = 0; m < RUNS; m += 2)
-                                head_norm_rope<2>(v + m, turned && n0 + 32 * m < p.k_end, s_hw + (n0 + 32 * m < p.q_cols ? 0 : 128), t, pos, p);
-                        }
-#pragma unroll
-                        for (int m = 0; m < RUNS; ++m)
-                            out[m] = make_uint4(pack2<F16>(v[m][0], v[m][1]), pack2<F16>(v[m][2], v[m][3]), pack2<F16>(v[m][4], v[m][5]),
-                                                pack2<F16>(v[m][6], v[m][7]));
-                    } else {
-                        convert(raw[0], hi, out);
-                    }
-                    uint16_t* yrows = ytile + first * p.ldy;
-                    if (whole) {
-#pragma unroll
-                        for (int m = 0; m < RUNS; ++m)
-                            if (row < p.M) *reinterpret_cast<uint4*>(yrows + r4 * p.ldy + 32 * m + 8 * t) = out[m];
-                    } else {
-                        // through 1 KB of shared memory, 64 columns at a time, written by consecutive lanes
-                        const uint32_t edge = smem_base + P::EDGE_OFFSET + static_cast<uint32_t>(warp - 4) * 1024u;
-                        const int rows = min(8, p.M - row0 - first);
-#pragma unroll
-                        for (int c = 0; c < CH; ++c) {
-                            __syncwarp();
-#pragma unroll
-                            for (int m = 0; m < 2; ++m)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(edge + r4 * 128 + m * 64 + t * 16), "r"(out[2 * c + m].x),
-                                             "r"(out[2 * c + m].y), "r"(out[2 * c + m].z), "r"(out[2 * c + m].w)
-                                             : "memory");
-                            __syncwarp();
-#pragma unroll 1
-                            for (int r = 0; r < rows; ++r)
-#pragma unroll
-                                for (int g = 0; g < 2; ++g) {
-                                    const int col = c * 64 + 32 * g + lane;
-                                    uint16_t e;
-                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(e) : "r"(edge + r * 128 + 64 * g + 2 * lane) : "memory");
-                                    if (n0 + col < p.N) yrows[r * p.ldy + col] = e;
-                                }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int c = 0; c < CH; ++c)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) raw[0][c][j] = raw[1][c][j];
             }
         }
     }
@@ -761,9 +774,8 @@ std::atomic<int> g_mx_tile{0};  // 0: chosen per call; 64 / 128: single CTAs wit
 // unit and warp there, a quantizer of its own about 1.5 us.  (K = 3072 -> 9216: 2 rows, 24 units, 6.1 against 6.6 us, 4 rows 7.1; 1152 -> 1152: 6 rows, 30
 // units, 4.7 against 5.5, 8 rows 5.2, 12 rows 6.3; 12288 -> 3072: 1 row, 48 units, 12.6 against 12.1.)
 constexpr int kFuseUnits = 32;
-template <int BN>
 bool fuse_fits(int M, int nkb) {
-    return static_cast<long long>(M) * nkb <= kFuseUnits && M <= 32 && nkb * ((M + 7) / 8 + 1) * 1024 <= MxPlan<BN, false, true>::RESIDENT;
+    return static_cast<long long>(M) * nkb <= kFuseUnits && M <= 32 && nkb * ((M + 7) / 8 + 1) * 1024 <= MxPlan<64, false, true>::RESIDENT;
 }
 
 // Columns per tile of single CTAs, or 512 for pairs: the shortest schedule, turns of the SMs x the time of a tile.  Microseconds a tile of nkb
@@ -791,7 +803,7 @@ dirotq_status_t set_mx_tile_columns(int columns) {
 
 bool mx_fuses(int M, int N, int nkb, const dirotq_qk_t* qk, int device) {
     const int plan = choose_plan(M, N, nkb, qk, sm_count(device));
-    return plan == 64 ? fuse_fits<64>(M, nkb) : plan == 128 ? fuse_fits<128>(M, nkb) : false;
+    return plan != 512 && fuse_fits(M, nkb);
 }
 
 dirotq_status_t launch_mx_gemm(const MxGemmArgs& a, cudaStream_t stream) {
