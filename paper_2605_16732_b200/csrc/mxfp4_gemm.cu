@@ -221,12 +221,13 @@ __device__ __forceinline__ void store_run(const MxKernelParams& p, int row0, int
     __syncwarp();
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(edge + r4 * 64 + t * 16), "r"(out.x), "r"(out.y), "r"(out.z), "r"(out.w) : "memory");
     __syncwarp();
-#pragma unroll 1
-    for (int r = 0; r < rows; ++r) {
-        uint16_t e;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(e) : "r"(edge + r * 64 + 2 * lane) : "memory");
-        if (n0 + lane < p.N) y[r * p.ldy + lane] = e;
-    }
+    uint16_t e[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(e[r]) : "r"(edge + r * 64 + 2 * lane) : "memory");
+    if (n0 + lane < p.N)
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < rows) y[r * p.ldy + lane] = e[r];
 }
 
 // Cosines and sines of four consecutive angles (`wide`: 16-byte aligned).
