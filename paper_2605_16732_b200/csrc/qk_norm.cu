@@ -37,29 +37,68 @@ struct QkParams {
     int L, per_warp, fold, part_sets, parts_q, parts_k, parts, items;
 };
 
-// Elements d0 .. + 3 and d1 .. + 3 of a head; SPLIT: two pieces (8 bytes each in 16 bits), else one (d1 = d0 + 4).
-template <typename T, bool SPLIT_PIECES>
-__device__ __forceinline__ Raw8<T> load_pieces(const T* head, int d0, int d1) {
+// How the elements of a head lie on its lanes and find their partners.
+enum Style {
+    PLAIN,    // no rotation: elements 8 sub + i of lane sub
+    PAIRS,    // the same; partners are neighbours
+    SPLIT,    // halves of the whole head: elements 4 sub + i and D/2 + 4 sub + i, i < 4: partners lie in one lane
+    QUARTER,  // halves of half a head: elements 2 sub + i, D/4 + 2 sub + i, i < 2, and, not turned, D/2 + 4 sub + i, i < 4
+    HALVES,   // halves of any other part of the head: as PAIRS, partners through shared memory
+};
+
+// A lane's eight elements of a head: one piece (16 bytes in 16 bits), or the two or three of its style, in the order of `element`.
+template <int STYLE>
+__device__ __forceinline__ int element(int i, int sub, int half) {
+    if (STYLE == SPLIT) return i < 4 ? 4 * sub + i : half + 4 * sub + i - 4;
+    if (STYLE == QUARTER) return i < 2 ? 2 * sub + i : i < 4 ? half + 2 * sub + i - 2 : 2 * half + 4 * sub + i - 4;
+    return 8 * sub + i;
+}
+template <typename T, int STYLE>
+__device__ __forceinline__ Raw8<T> load_pieces(const T* head, int sub, int half) {
     Raw8<T> r;
-    if constexpr (sizeof(T) == 4) {
+    const int d0 = element<STYLE>(0, sub, half), d2 = element<STYLE>(2, sub, half), d4 = element<STYLE>(4, sub, half);
+    uint32_t* w = reinterpret_cast<uint32_t*>(&r);
+    if constexpr (STYLE == QUARTER) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(head + d0);
+            *reinterpret_cast<uint2*>(w + 2) = *reinterpret_cast<const uint2*>(head + d2);
+            *reinterpret_cast<uint4*>(w + 4) = *reinterpret_cast<const uint4*>(head + d4);
+        } else {
+            w[0] = *reinterpret_cast<const uint32_t*>(head + d0);
+            w[1] = *reinterpret_cast<const uint32_t*>(head + d2);
+            *reinterpret_cast<uint2*>(w + 2) = *reinterpret_cast<const uint2*>(head + d4);
+        }
+    } else if constexpr (sizeof(T) == 4) {
         r.u[0] = *reinterpret_cast<const uint4*>(head + d0);
-        r.u[1] = *reinterpret_cast<const uint4*>(head + d1);
-    } else if constexpr (SPLIT_PIECES) {
-        const uint2 a = *reinterpret_cast<const uint2*>(head + d0), b = *reinterpret_cast<const uint2*>(head + d1);
-        r.u[0] = make_uint4(a.x, a.y, b.x, b.y);
+        r.u[1] = *reinterpret_cast<const uint4*>(head + d4);
+    } else if constexpr (STYLE == SPLIT) {
+        *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(head + d0);
+        *reinterpret_cast<uint2*>(w + 2) = *reinterpret_cast<const uint2*>(head + d4);
     } else {
         r.u[0] = *reinterpret_cast<const uint4*>(head + d0);
     }
     return r;
 }
-template <typename T, bool SPLIT_PIECES>
-__device__ __forceinline__ void store_pieces(T* head, int d0, int d1, const Raw8<T>& r) {
-    if constexpr (sizeof(T) == 4) {
+template <typename T, int STYLE>
+__device__ __forceinline__ void store_pieces(T* head, int sub, int half, const Raw8<T>& r) {
+    const int d0 = element<STYLE>(0, sub, half), d2 = element<STYLE>(2, sub, half), d4 = element<STYLE>(4, sub, half);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
+    if constexpr (STYLE == QUARTER) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<uint2*>(head + d0) = *reinterpret_cast<const uint2*>(w);
+            *reinterpret_cast<uint2*>(head + d2) = *reinterpret_cast<const uint2*>(w + 2);
+            *reinterpret_cast<uint4*>(head + d4) = *reinterpret_cast<const uint4*>(w + 4);
+        } else {
+            *reinterpret_cast<uint32_t*>(head + d0) = w[0];
+            *reinterpret_cast<uint32_t*>(head + d2) = w[1];
+            *reinterpret_cast<uint2*>(head + d4) = *reinterpret_cast<const uint2*>(w + 2);
+        }
+    } else if constexpr (sizeof(T) == 4) {
         *reinterpret_cast<uint4*>(head + d0) = r.u[0];
-        *reinterpret_cast<uint4*>(head + d1) = r.u[1];
-    } else if constexpr (SPLIT_PIECES) {
-        *reinterpret_cast<uint2*>(head + d0) = make_uint2(r.u[0].x, r.u[0].y);
-        *reinterpret_cast<uint2*>(head + d1) = make_uint2(r.u[0].z, r.u[0].w);
+        *reinterpret_cast<uint4*>(head + d4) = r.u[1];
+    } else if constexpr (STYLE == SPLIT) {
+        *reinterpret_cast<uint2*>(head + d0) = *reinterpret_cast<const uint2*>(w);
+        *reinterpret_cast<uint2*>(head + d4) = *reinterpret_cast<const uint2*>(w + 2);
     } else {
         *reinterpret_cast<uint4*>(head + d0) = r.u[0];
     }
@@ -75,14 +114,6 @@ __device__ __forceinline__ float weight_at(const void* p, int i, int dtype) {
 template <typename T>
 constexpr int kHeads = sizeof(T) == 4 ? 2 : 4;  // sets of heads a warp takes at once
 
-// How the elements of a head lie on its lanes and find their partners.
-enum Style {
-    PLAIN,   // no rotation: element d0 + i of lane sub, d0 = 8 sub
-    PAIRS,   // the same; partners are neighbours
-    SPLIT,   // halves of the whole head: elements 4 sub + i and D/2 + 4 sub + i, i < 4: partners lie in one lane
-    HALVES,  // halves of a part of the head, of any length: as PAIRS, partners through shared memory
-};
-
 // STYLE; LANES: lanes of a head where head_dim is 64, 72 or 128, 0: p.L, any.
 template <typename T, int STYLE, int LANES>
 __global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 2 : 3) qk_norm_rope_kernel(const __grid_constant__ QkParams p) {
@@ -96,8 +127,6 @@ __global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 
     const int head0 = lane - sub;                  // the lane that holds the head's first elements
     const bool lives = 32 % (LANES ? LANES : 1) == 0 && LANES ? true : in_warp < per_warp;
     const int half = p.rot >> 1;
-    const int d0 = STYLE == SPLIT ? 4 * sub : 8 * sub, d1 = STYLE == SPLIT ? half + 4 * sub : d0 + 4;  // elements d0 + i, d1 + i, i < 4
-    auto element = [&](int i) { return i < 4 ? d0 + i : d1 + i - 4; };
     // HALVES: where the partners of this lane's elements will lie; the spare ninth word holds the zero that what is not turned takes instead (an
     // infinity in some partner's place would leave NaN)
     float* const s_mine = &s_head[STYLE == HALVES ? warp : 0][lane * PITCH];
@@ -106,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 
         s_mine[8] = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int d = d0 + i, from = d < half ? d + half : d - half;
+            const int d = 8 * sub + i, from = d < half ? d + half : d - half;
             s_partner[i] = lives && d < p.rot ? &s_head[warp][(head0 + (from >> 3)) * PITCH + (from & 7)] : s_mine + 8;
         }
     }
@@ -136,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 
             for (int j = 0; j < HEADS; ++j) {
                 const int h = h0 + j * per_warp + in_warp;
                 raw[j] = Raw8<T>();
-                if (lives && h < h_end) raw[j] = load_pieces<T, STYLE == SPLIT>(from + h * p.D, d0, d1);
+                if (lives && h < h_end) raw[j] = load_pieces<T, STYLE>(from + h * p.D, sub, half);
             }
         };
         load_set();
@@ -153,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 
 #pragma unroll
                 for (int j = 0; j < HEADS; ++j) {
                     const int h = h0 + j * per_warp + in_warp;
-                    if (lives && h < h_end) store_pieces<T, STYLE == SPLIT>(out + h * p.D, d0, d1, raw[j]);
+                    if (lives && h < h_end) store_pieces<T, STYLE>(out + h * p.D, sub, half, raw[j]);
                 }
                 if ((h0 += set) >= h_end) break;
                 load_set();
@@ -164,26 +193,31 @@ __global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 
         // into the token's cosines (c) and sines (s) once for all its heads.  (Where nothing is turned c = w and s = 0.)
         float c[8], s[8];
         {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                c[i] = 1.f;
+                s[i] = 0.f;
+            }
             if constexpr (STYLE != PLAIN) {
                 const float* cs = p.cos_table + static_cast<long long>(pos) * p.ld_table;
                 const float* sn = p.sin_table + static_cast<long long>(pos) * p.ld_table;
-                if (p.wide_table && lives && (STYLE == PAIRS || STYLE == SPLIT) && d0 + 8 <= p.rot + (STYLE == SPLIT ? 8 : 0)) {
-                    const int a = STYLE == PAIRS ? d0 >> 1 : d0;
-                    const float4 c0 = __ldg(reinterpret_cast<const float4*>(cs + a)), s0 = __ldg(reinterpret_cast<const float4*>(sn + a));
+                auto pair = [&](int first, int second, float cv, float sv) {  // these two of the lane's elements are one pair
+                    c[first] = c[second] = cv;
+                    s[first] = -sv;
+                    s[second] = sv;
+                };
+                if ((STYLE == SPLIT || (STYLE == PAIRS && 8 * sub + 8 <= p.rot)) && p.wide_table && lives) {
+                    const float4 c0 = __ldg(reinterpret_cast<const float4*>(cs + 4 * sub)), s0 = __ldg(reinterpret_cast<const float4*>(sn + 4 * sub));
                     const float cv[4] = {c0.x, c0.y, c0.z, c0.w}, sv[4] = {s0.x, s0.y, s0.z, s0.w};
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int a0 = STYLE == PAIRS ? 2 * k : k, a1 = STYLE == PAIRS ? 2 * k + 1 : k + 4;
-                        c[a0] = c[a1] = cv[k];
-                        s[a0] = -sv[k];
-                        s[a1] = sv[k];
-                    }
+                    for (int k = 0; k < 4; ++k) pair(STYLE == PAIRS ? 2 * k : k, STYLE == PAIRS ? 2 * k + 1 : k + 4, cv[k], sv[k]);
+                } else if (STYLE == QUARTER && lives) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) pair(k, k + 2, __ldg(cs + 2 * sub + k), __ldg(sn + 2 * sub + k));
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int d = element(i);
-                        c[i] = 1.f;
-                        s[i] = 0.f;
+                        const int d = element<STYLE>(i, sub, half);
                         if (lives && d < p.rot) {
                             const int a = STYLE == PAIRS ? d >> 1 : d < half ? d : d - half;
                             const bool second = STYLE == PAIRS ? (d & 1) != 0 : d >= half;
@@ -192,21 +226,20 @@ __global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 
                         }
                     }
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) c[i] = 1.f;
             }
             if (weighted && lives) {
                 const float* w = s_w[kind];
-                const float4 w0 = *reinterpret_cast<const float4*>(w + d0), w1 = *reinterpret_cast<const float4*>(w + d1);
-                const float wv[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+                float wv[8];
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) *reinterpret_cast<float2*>(wv + i) = *reinterpret_cast<const float2*>(w + element<STYLE>(i, sub, half));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     c[i] *= wv[i];
                     if constexpr (STYLE == PAIRS) s[i] *= wv[i ^ 1];
                     if constexpr (STYLE == SPLIT) s[i] *= wv[i ^ 4];
+                    if constexpr (STYLE == QUARTER) s[i] *= i < 4 ? wv[i ^ 2] : 0.f;
                     if constexpr (STYLE == HALVES) {
-                        const int d = element(i);
+                        const int d = 8 * sub + i;
                         s[i] *= w[d >= p.rot ? d : d < half ? d + half : d - half];
                     }
                 }
@@ -243,13 +276,13 @@ __global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 
                 for (int i = 0; i < 8; ++i) o[i] = r * (v[i] * c[i]);
             } else {
                 float partner[8];
-                if constexpr (STYLE == PAIRS || STYLE == SPLIT) {
+                if constexpr (STYLE == PAIRS || STYLE == SPLIT || STYLE == QUARTER) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) partner[i] = v[STYLE == PAIRS ? i ^ 1 : i ^ 4];
+                    for (int i = 0; i < 8; ++i) partner[i] = STYLE == QUARTER && i >= 4 ? 0.f : v[STYLE == PAIRS ? i ^ 1 : STYLE == SPLIT ? i ^ 4 : i ^ 2];
                     if (STYLE == PAIRS && p.rot != p.D) {  // what has no partner takes nothing of one (an infinity there would leave NaN)
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            if (d0 + i >= p.rot) partner[i] = 0.f;
+                            if (8 * sub + i >= p.rot) partner[i] = 0.f;
                     }
                 } else {
                     __syncwarp();
@@ -262,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = r * fmaf(partner[i], s[i], v[i] * c[i]);
             }
-            if (lives && h < h_end) store_pieces<T, STYLE == SPLIT>(out + h * p.D, d0, d1, pack8<T>(o));
+            if (lives && h < h_end) store_pieces<T, STYLE>(out + h * p.D, sub, half, pack8<T>(o));
         }
         if ((h0 += set) >= h_end) break;
         load_set();
@@ -300,6 +333,7 @@ cudaError_t launch_t(QkParams& p, int M, cudaStream_t stream) {
     return p.rope == DIROTQ_ROPE_NONE    ? DIROTQ_QK_STYLE(PLAIN)
            : p.rope == DIROTQ_ROPE_PAIRS ? DIROTQ_QK_STYLE(PAIRS)
            : p.rot == p.D                ? DIROTQ_QK_STYLE(SPLIT)
+           : 2 * p.rot == p.D            ? DIROTQ_QK_STYLE(QUARTER)
                                          : DIROTQ_QK_STYLE(HALVES);
 #undef DIROTQ_QK_STYLE
 }

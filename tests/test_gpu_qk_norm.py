@@ -46,7 +46,9 @@ def _within(y, want, tol):
 CASES = [  # M, q heads, kv heads, head_dim, rotated, style
     (1, 1, 1, 8, 8, "pairs"), (1, 32, 8, 128, 128, "halves"), (3, 5, 5, 64, 64, "pairs"), (7, 16, 16, 72, 36, "halves"), (7, 16, 16, 72, 72, "halves"),
     (33, 14, 2, 128, 64, "pairs"), (5, 3, 1, 256, 256, "halves"), (64, 24, 24, 128, 128, "pairs"), (9, 6, 3, 96, 2, "pairs"), (4, 4, 4, 32, 16, "halves"),
-    (11, 7, 1, 40, 0, None), (300, 8, 2, 160, 80, "halves"), (2, 9, 9, 24, 24, "pairs")]
+    (11, 7, 1, 40, 0, None), (300, 8, 2, 160, 80, "halves"), (2, 9, 9, 24, 24, "pairs"),
+    (6, 4, 2, 8, 4, "halves"), (5, 3, 3, 64, 32, "halves"), (3, 4, 1, 128, 64, "halves"), (4, 2, 2, 128, 48, "halves"), (3, 2, 1, 72, 10, "halves"), (400, 16, 16, 72, 36, "halves"), (2500, 3, 2, 16, 8, "halves"),
+    (2600, 5, 1, 128, 128, "pairs")]
 
 
 @pytest.mark.parametrize("M,hq,hk,D,rot,style", CASES)
