@@ -38,12 +38,17 @@ constexpr int GROUP_THREADS = EPI_WARPS * 16;  // of one of the two epilogue gro
 template <int BN, bool PAIR, bool FUSE>
 struct MxPlan {
     static constexpr int NB = BN == 256 ? 2 : 1;                              // 128-column blocks whose scales a stage holds
+    // k-blocks per stage: two where a k-block is little work, so that a short call pays for the roles' waits and hand-overs half as often
+    // (128 rows, 12288 -> 3072: 9.6 against 10.3 us; 16 rows, 3072 -> 9216: 6.4 against 6.9 with the quantizer).  What is left at 64 columns,
+    // 0.15 us a k-block, is its four MMAs, each of which waits for the one before: they add to the same accumulator in order.
+    static constexpr int KBS = BN == 64 || FUSE ? 2 : 1;
     static constexpr int A_STAGE = FUSE ? 0 : A_BYTES;
     static constexpr int B_BYTES = (PAIR ? BN / 2 : BN) * 128;                // this CTA's rows of b: the tile's (single) or half of them (pair)
-    static constexpr int SF_OFFSET = A_STAGE + B_BYTES;                       // scales of a (unless they stay), then of b
-    static constexpr int SFB_OFFSET = SF_OFFSET + (FUSE ? 0 : ATOMS);
-    static constexpr int STAGE_BYTES = SFB_OFFSET + NB * ATOMS;               // pair 35 KB, single 34 / 26 KB, fused 17 / 9 KB
-    static constexpr int STAGES = FUSE ? (BN == 64 ? 16 : 8) : (BN == 64 ? 8 : 6);
+    static constexpr int B_OFFSET = KBS * A_STAGE;
+    static constexpr int SF_OFFSET = B_OFFSET + KBS * B_BYTES;                // scales of a (unless they stay), then of b
+    static constexpr int SFB_OFFSET = SF_OFFSET + (FUSE ? 0 : KBS * ATOMS);
+    static constexpr int STAGE_BYTES = SFB_OFFSET + KBS * NB * ATOMS;         // pair 35 KB, single 34 / 52 KB, fused 34 / 18 KB
+    static constexpr int STAGES = FUSE ? (BN == 64 ? 8 : 4) : (BN == 64 ? 4 : 6);
     static constexpr int RESIDENT = FUSE ? 64 * 1024 : 0;                     // codes and scales of the activations (see kFuseUnits)
     static constexpr int BAR_OFFSET = RESIDENT + STAGES * STAGE_BYTES;
     static constexpr int BIAS_OFFSET = BAR_OFFSET + 512;                      // per epilogue group two buffers of 128 values
@@ -52,10 +57,10 @@ struct MxPlan {
     static constexpr int SUM_OFFSET = EDGE_OFFSET + EPI_WARPS * 512;          // sums of squares of 32 rows per epilogue warp
     static constexpr int SMEM_BYTES = SUM_OFFSET + EPI_WARPS * 128 + 1024;
     static constexpr int ACC_BUFS = PAIR ? 1 : 2;
-    static constexpr int TMEM_SF = ACC_BUFS * BN;                             // columns of the scales: per stage 8 for a, 8 per 128 columns
+    static constexpr int TMEM_SF = ACC_BUFS * BN;                             // columns of the scales: per k-block 8 for a, 8 per 128 columns
     static constexpr int SF_COLS = 8 * (1 + NB);
     static_assert(PAIR ? BN == 256 && !FUSE : BN == 128 || BN == 64, "plans");
-    static_assert(TMEM_SF + STAGES * SF_COLS <= 512, "tensor memory plan");
+    static_assert(TMEM_SF + STAGES * KBS * SF_COLS <= 512, "tensor memory plan");
     static_assert(8 * ((PAIR ? 4 : 3) * STAGES + 5) <= 480, "barriers end below the words at +480");
     static_assert(SMEM_BYTES <= 232448, "shared memory plan");
     static_assert(STAGE_BYTES % 1024 == 0, "operand tiles must stay 1024-byte aligned");
@@ -417,7 +422,7 @@ template <int BN, bool PAIR, bool QKV, bool F16, bool FUSE>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ MxKernelParams p) {
     using P = MxPlan<BN, PAIR, FUSE>;
-    constexpr int NB = P::NB, STAGES = P::STAGES, ACC_BUFS = P::ACC_BUFS, STAGE_BYTES = P::STAGE_BYTES;
+    constexpr int NB = P::NB, STAGES = P::STAGES, ACC_BUFS = P::ACC_BUFS, STAGE_BYTES = P::STAGE_BYTES, KBS = P::KBS;
     constexpr int CW = PAIR ? 128 : BN;  // columns of an epilogue group
     constexpr bool SPLIT_REGS = QKV || CW == 128;
     extern __shared__ uint8_t smem_raw[];
@@ -487,37 +492,50 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             RingPos<STAGES> at;
             bool ok = true;
             int early = 0;  // stages of the first tile whose rows of b are already on their way
+            // k-blocks kb .. of a stage that exist (KBS, but for the last of an odd number)
             auto load_a = [&](int m_blk, int kb, uint32_t st, uint32_t bar) {
-                tma_load_2d(st, &tmap_a, bar, kb * 128, m_blk * BM);  // byte coordinates; rows past M are filled with zeros and still counted
-                bulk_load(st + P::SF_OFFSET, p.asf + ((static_cast<size_t>(m_blk >> 1) * p.nkb + kb) * 2 + (m_blk & 1)) * ATOMS, ATOMS, bar);
+#pragma unroll
+                for (int j = 0; j < KBS; ++j)
+                    if (j == 0 || kb + j < p.nkb) {
+                        tma_load_2d(st + j * P::A_STAGE, &tmap_a, bar, (kb + j) * 128, m_blk * BM);  // byte coordinates; rows past M: zeros, counted
+                        bulk_load(st + P::SF_OFFSET + j * ATOMS, p.asf + ((static_cast<size_t>(m_blk >> 1) * p.nkb + kb + j) * 2 + (m_blk & 1)) * ATOMS, ATOMS,
+                                  bar);
+                    }
             };
             auto load_b = [&](int n_blk, int kb, uint32_t st, uint32_t bar) {
-                tma_load_2d(st + P::A_STAGE, &tmap_b, bar, kb * 128, n_blk * BN + (PAIR ? static_cast<int>(cta_rank) * 128 : 0));
                 const int rb = n_blk * BN / 128;  // (the atoms of 256 rows always exist)
-                bulk_load(st + P::SFB_OFFSET, p.bsf + ((static_cast<size_t>(rb >> 1) * p.nkb + kb) * 2 + (rb & 1)) * ATOMS, NB * ATOMS, bar);
+#pragma unroll
+                for (int j = 0; j < KBS; ++j)
+                    if (j == 0 || kb + j < p.nkb) {
+                        tma_load_2d(st + P::B_OFFSET + j * P::B_BYTES, &tmap_b, bar, (kb + j) * 128, n_blk * BN + (PAIR ? static_cast<int>(cta_rank) * 128 : 0));
+                        bulk_load(st + P::SFB_OFFSET + j * NB * ATOMS, p.bsf + ((static_cast<size_t>(rb >> 1) * p.nkb + kb + j) * 2 + (rb & 1)) * ATOMS,
+                                  NB * ATOMS, bar);
+                    }
             };
-            const uint32_t stage_tx = ((FUSE ? 0 : p.a_box) + p.b_box) * 128 + (NB + (FUSE ? 0 : 1)) * ATOMS;
+            auto stage_tx = [&](int kb) {
+                return min(KBS, p.nkb - kb) * (((FUSE ? 0 : p.a_box) + p.b_box) * 128 + (NB + (FUSE ? 0 : 1)) * ATOMS);
+            };
             if (!FUSE && p.early && tile_first < num_tiles) {
                 // the previous kernel is this call's own quantizer, which does not write b: b's first stages land while it runs
-                early = min(STAGES, p.nkb);
+                early = min(STAGES, (p.nkb + KBS - 1) / KBS);
                 if (elect_one())
-                    for (int kb = 0; kb < early; ++kb) {
-                        mbar_arrive_expect_tx(full_bar(kb), stage_tx);
-                        load_b(tile_first / num_m_blocks, kb, ring + kb * STAGE_BYTES, full_bar(kb));
+                    for (int i = 0; i < early; ++i) {
+                        mbar_arrive_expect_tx(full_bar(i), stage_tx(i * KBS));
+                        load_b(tile_first / num_m_blocks, i * KBS, ring + i * STAGE_BYTES, full_bar(i));
                     }
                 __syncwarp();
             }
             grid_dependency_wait();
             for (int tile = tile_first; ok && tile < num_tiles; tile += tile_step) {
                 const int m_blk = (tile % num_m_blocks) * (PAIR ? 2 : 1) + static_cast<int>(cta_rank), n_blk = tile / num_m_blocks;
-                for (int kb = 0; kb < p.nkb; ++kb, at.next()) {
+                for (int kb = 0; kb < p.nkb; kb += KBS, at.next()) {
                     const uint32_t s = at.s;
                     if (!mbar_wait(empty_bar(s), at.ph ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER)) { ok = false; break; }
                     const uint32_t st = ring + s * STAGE_BYTES;
                     if (!elect_one()) continue;
                     const bool begun = !FUSE && static_cast<int>(at.it) < early;
                     if (!begun) {
-                        mbar_arrive_expect_tx(full_bar(s), stage_tx);
+                        mbar_arrive_expect_tx(full_bar(s), stage_tx(kb));
                         load_b(n_blk, kb, st, full_bar(s));
                     }
                     if constexpr (!FUSE) load_a(m_blk, kb, st, full_bar(s));
@@ -547,20 +565,24 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
                     const uint32_t d = tmem_base + acc * BN;
                     // a 64-column tile's scales are one half of its 128-column block's: rows 0..63 lie in an atom's first two columns of tensor memory
                     const uint32_t half = BN == 64 ? 2 * ((tile / num_m_blocks) & 1) : 0;
-                    for (int kb = 0; kb < p.nkb; ++kb, at.next()) {
+                    for (int kb = 0; kb < p.nkb; kb += KBS, at.next()) {
                         const uint32_t s = at.s;
                         // (the copier warps have seen the stage's loads land, in both CTAs of a pair: their barrier covers the operands)
                         if (!mbar_wait(sfready_bar(s), at.ph, abort_flag, p.status, DEV_TIMEOUT_MMA)) { ok = false; break; }
                         tc_fence_after_sync();
-                        const uint32_t tsf = tmem_base + P::TMEM_SF + s * P::SF_COLS;
                         const uint64_t sdesc = desc0 + s * (STAGE_BYTES >> 4);
-                        const uint64_t adesc = FUSE ? xdesc + static_cast<uint32_t>(kb * p.groups * (1024 >> 4)) : sdesc;
-                        const uint64_t bdesc = sdesc + (P::A_STAGE >> 4);
                         if (!elect_one()) continue;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)  // K = 64 elements = 32 bytes per instruction
-                            umma_mxf4<PAIR>(d, adesc + 2 * k, bdesc + 2 * k, (k & 1) ? idesc1 : idesc0, tsf + 4 * (k >> 1), tsf + 8 + 4 * NB * (k >> 1) + half,
-                                            (kb | k) != 0);
+                        for (int j = 0; j < KBS; ++j)
+                            if (j == 0 || kb + j < p.nkb) {
+                                const uint32_t tsf = tmem_base + P::TMEM_SF + (s * KBS + j) * P::SF_COLS;
+                                const uint64_t adesc = FUSE ? xdesc + static_cast<uint32_t>((kb + j) * p.groups * (1024 >> 4)) : sdesc + j * (P::A_STAGE >> 4);
+                                const uint64_t bdesc = sdesc + (P::B_OFFSET >> 4) + j * (P::B_BYTES >> 4);
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)  // K = 64 elements = 32 bytes per instruction
+                                    umma_mxf4<PAIR>(d, adesc + 2 * k, bdesc + 2 * k, (k & 1) ? idesc1 : idesc0, tsf + 4 * (k >> 1),
+                                                    tsf + 8 + 4 * NB * (k >> 1) + half, (kb | j | k) != 0);
+                            }
                         if constexpr (PAIR) umma_commit_pair(empty_bar(s), 3);
                         else umma_commit(empty_bar(s));
                     }
@@ -576,7 +598,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             bool ok = true;
             if constexpr (FUSE) ok = mbar_wait(xready_bar, 0, abort_flag, p.status, DEV_TIMEOUT_UNPACK);
             for (int tile = tile_first; ok && tile < num_tiles; tile += tile_step) {
-                for (int kb = 0; kb < p.nkb; ++kb, at.next()) {
+                for (int kb = 0; kb < p.nkb; kb += KBS, at.next()) {
                     const uint32_t s = at.s;
                     if (!mbar_wait(full_bar(s), at.ph, abort_flag, p.status, DEV_TIMEOUT_UNPACK)) { ok = false; break; }
                     if constexpr (PAIR) {
@@ -587,21 +609,25 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
                         if (!mbar_wait(peer_bar(s), at.ph, abort_flag, p.status, DEV_TIMEOUT_UNPACK)) { ok = false; break; }
                     }
                     tc_fence_after_sync();
-                    const uint32_t sfa = FUSE ? smem_base + p.nkb * p.groups * 1024 + kb * ATOMS : ring + s * STAGE_BYTES + P::SF_OFFSET;
-                    const uint32_t sfb = ring + s * STAGE_BYTES + P::SFB_OFFSET;
-                    const uint32_t tsf = tmem_base + P::TMEM_SF + s * P::SF_COLS;
                     if (!elect_one()) continue;
-                    // atom i of a at column 4 i; atom i of column block b at 8 + 4 NB i + 4 b (the blocks of a tile side by side)
-                    if (warp == 2) {
-                        sf_copy<PAIR>(tsf, sf_desc(sfa));
-                        sf_copy<PAIR>(tsf + 4, sf_desc(sfa + 512));
-                        if constexpr (NB == 2) sf_copy<PAIR>(tsf + 8, sf_desc(sfb));
-                    } else {
-                        if constexpr (NB == 1) sf_copy<PAIR>(tsf + 8, sf_desc(sfb));
-                        if constexpr (NB == 2) sf_copy<PAIR>(tsf + 12, sf_desc(sfb + ATOMS));
 #pragma unroll
-                        for (int b = 0; b < NB; ++b) sf_copy<PAIR>(tsf + 8 + 4 * NB + 4 * b, sf_desc(sfb + b * ATOMS + 512));
-                    }
+                    for (int j = 0; j < KBS; ++j)
+                        if (j == 0 || kb + j < p.nkb) {
+                            const uint32_t sfa = FUSE ? smem_base + p.nkb * p.groups * 1024 + (kb + j) * ATOMS : ring + s * STAGE_BYTES + P::SF_OFFSET + j * ATOMS;
+                            const uint32_t sfb = ring + s * STAGE_BYTES + P::SFB_OFFSET + j * NB * ATOMS;
+                            const uint32_t tsf = tmem_base + P::TMEM_SF + (s * KBS + j) * P::SF_COLS;
+                            // atom i of a at column 4 i; atom i of column block b at 8 + 4 NB i + 4 b (the blocks of a tile side by side)
+                            if (warp == 2) {
+                                sf_copy<PAIR>(tsf, sf_desc(sfa));
+                                sf_copy<PAIR>(tsf + 4, sf_desc(sfa + 512));
+                                if constexpr (NB == 2) sf_copy<PAIR>(tsf + 8, sf_desc(sfb));
+                            } else {
+                                if constexpr (NB == 1) sf_copy<PAIR>(tsf + 8, sf_desc(sfb));
+                                if constexpr (NB == 2) sf_copy<PAIR>(tsf + 12, sf_desc(sfb + ATOMS));
+#pragma unroll
+                                for (int b = 0; b < NB; ++b) sf_copy<PAIR>(tsf + 8 + 4 * NB + 4 * b, sf_desc(sfb + b * ATOMS + 512));
+                            }
+                        }
                     if constexpr (PAIR) umma_commit_pair(sfready_bar(s), 1);  // the leader's barrier only
                     else umma_commit(sfready_bar(s));
                 }

@@ -44,7 +44,7 @@ def _householder(K: int, seed: int) -> torch.Tensor:
     return torch.eye(K, dtype=torch.float64, device="cuda") - 2.0 * torch.outer(v, v)
 
 
-FMT = "int4"  # set from --fmt: "int4" (groups of G, bf16 scales) or "nvfp4" (blocks of 16, E4M3 scales)
+FMT = "int4"  # set from --fmt: "int4" (groups of G, bf16 scales), "nvfp4" (blocks of 16, E4M3 scales), ..., or "mxfp4" (no rotation)
 
 
 class Case:
@@ -53,7 +53,14 @@ class Case:
         spec = synth.LayerSpec(K=K, N=N, r=r, G=G if FMT in ("int4", "int4_asym", "int4_ph") else 64, model=model, seed=7)
         W, bias = synth.make_weights(spec)
         self.x = _bf(synth.make_tokens(spec, M, batch_seed=11))
-        Wd, Q = torch.from_numpy(W).cuda(), _householder(K, K + r)
+        self.y = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+        Wd = torch.from_numpy(W).cuda()
+        self.Wb = Wd.to(torch.bfloat16)
+        if FMT == "mxfp4":
+            self.layer = dq.dirotq_mxfp4_quantize(Wd, layout=dq.LAYOUT_KN)
+            self.ws, self.bias, self.xq = dq.alloc_mxfp4_workspace(M, K), _bf(bias), dq.dirotq_mxfp4_alloc(M, K)
+            return
+        Q = _householder(K, K + r)
         if FMT == "nvfp4":
             # calibrate the activations' power-of-two scale on this batch through the library's own rotation
             probe = dq.dirotq_prepare_layer_nvfp4(Wd, Q, r, 0, bias=_bf(bias))
@@ -74,12 +81,25 @@ class Case:
             self.layer = dq.dirotq_prepare_layer_nvfp4_ph(Wd, Uh, dq.dirotq_act_scale_log2_ph(self.x[:1024].contiguous(), Uh), bias=_bf(bias))
         else:
             self.layer = dq.dirotq_prepare_layer(Wd, Q, r, G, bias=_bf(bias))
-        self.y = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
         self.ws = dq.alloc_workspace(self.layer, M)
-        self.Wb = (torch.from_numpy(W).cuda()).to(torch.bfloat16)
 
     def run(self):
-        dq.dirotq_linear(self.x, self.layer, self.y, self.ws)
+        if FMT == "mxfp4":
+            dq.dirotq_mxfp4_linear(self.x, self.layer, self.y, self.ws, bias=self.bias)
+        else:
+            dq.dirotq_linear(self.x, self.layer, self.y, self.ws)
+
+    def first(self):
+        if FMT == "mxfp4":
+            dq.dirotq_mxfp4_quantize(self.x, out=self.xq)
+        else:
+            dq.dirotq_rotate_quantize(self.x, self.layer, self.ws)
+
+    def second(self):
+        if FMT == "mxfp4":
+            dq.dirotq_mxfp4_gemm(self.xq, self.layer, self.y, self.ws, bias=self.bias)
+        else:
+            dq.dirotq_w4a4_gemm(self.M, self.layer, self.ws, self.y)
 
     def time_kernels(self, iters):
         for _ in range(3):
@@ -88,9 +108,9 @@ class Case:
         for _ in range(iters):
             a, b, c = (torch.cuda.Event(enable_timing=True) for _ in range(3))
             a.record()
-            dq.dirotq_rotate_quantize(self.x, self.layer, self.ws)
+            self.first()
             b.record()
-            dq.dirotq_w4a4_gemm(self.M, self.layer, self.ws, self.y)
+            self.second()
             c.record()
             torch.cuda.synchronize()
             rot.append(a.elapsed_time(b))
@@ -135,14 +155,18 @@ class Case:
     def report(self, tag, iters, p_bf16, hbm, graphs=False):
         rot, gem, cb = self.time_kernels(iters)
         M, K, N, r, G = self.M, self.K, self.N, self.r, self.G
-        PH, NV = FMT in ("int4_ph", "nvfp4_ph"), FMT in ("nvfp4", "nvfp4_ph")
+        PH, NV, MX = FMT in ("int4_ph", "nvfp4_ph"), FMT in ("nvfp4", "nvfp4_ph", "mxfp4"), FMT == "mxfp4"
+        if MX:  # no rotation and no 16-bit part
+            r, G = 0, 32
         K_l = K if PH else K - r
         n_g = -(-K_l // G) if G else 1
         tot = rot + gem
         p_i8 = (4.0 if NV else 2.0) * p_bf16  # nominal ratio of the 4-bit / 8-bit tensor peak to bf16
-        first_flops = 4.0 * M * K * max(64, -(-r // 64) * 64) if PH else 2.0 * M * K * K
+        first_flops = 0.0 if MX else 4.0 * M * K * max(64, -(-r // 64) * 64) if PH else 2.0 * M * K * K
         t_roof = (2.0 * M * K_l * N / p_i8 + (first_flops + 2.0 * M * r * N) / p_bf16) / 1e12 * 1e3
-        if FMT == "w4a8":
+        if MX:
+            bytes_alg = 2 * M * K + 17 / 32 * (2 * M * K + K * N) + 2 * N + 2 * M * N
+        elif FMT == "w4a8":
             bytes_alg = 2 * M * K + 2 * K * K + K_l * N / 2 + 4 * N + 2 * 64 * N + 2 * (M * K_l * 5 + 8 * M + 2 * M * 64) + 2 * M * N
         elif NV:
             bytes_alg = 2 * M * K + 2 * K * K + K_l * N / 2 + K_l / 16 * N + 2 * 64 * N + 2 * (M * K_l / 2 + M * K_l / 16 + 2 * M * 64) + 2 * M * N
@@ -241,9 +265,9 @@ def memory_report():
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--memory", action="store_true", help="print the layer sizes (no GPU needed) and exit")
-    ap.add_argument("--configs", default="1,2,4,5", help="comma-separated subset of 1,2,3p,4,5")
+    ap.add_argument("--configs", default="1,2,4,5", help="comma-separated subset of 1,2,3p,4,5,qkv")
     ap.add_argument("--iters", type=int, default=20)
-    ap.add_argument("--fmt", default="int4", choices=["int4", "nvfp4", "int4_asym", "w4a8", "int4_ph", "nvfp4_ph"])
+    ap.add_argument("--fmt", default="int4", choices=["int4", "nvfp4", "int4_asym", "w4a8", "int4_ph", "nvfp4_ph", "mxfp4"])
     ap.add_argument("--ranks", default="16,32,64,128", help="ranks swept by config 4")
     args = ap.parse_args()
     if args.memory:
@@ -304,6 +328,21 @@ def main():
                     c.report("4: FLUX batch 4 (M=18432) rank/group sweep", max(5, args.iters // 2), p_bf16, hbm)
                     c.close()
                     torch.cuda.empty_cache()
+    if "qkv" in todo:
+        # a fused q/k/v projection of 24 heads of 128 with the norm and rotation of q and k: in the product's epilogue (mxfp4), or behind the
+        # layer; alone, and behind the same tokens' projection
+        M, K, heads, D = 4608, 3072, 24, 128
+        c = Case(M, K, 3 * heads * D, 32, 64, synth.FLUX)
+        angle = torch.arange(M, device="cuda")[:, None] * 10000.0 ** (-torch.arange(0, D, 2, device="cuda") / D)
+        one = torch.ones(D, device="cuda", dtype=torch.bfloat16)
+        qk = dq.QkNorm(heads, heads, D, q_weight=one, k_weight=one, rope="pairs", cos=angle.cos().contiguous(), sin=angle.sin().contiguous())
+        q, k = (torch.empty((M, heads * D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        fused = (lambda: dq.dirotq_mxfp4_qkv(c.x, c.layer, c.y, c.ws, qk, bias=c.bias)) if FMT == "mxfp4" else \
+            (lambda: dq.dirotq_linear_qkv(c.x, c.layer, c.y, c.ws, qk))
+        print(json.dumps({"config": "qkv: FLUX-shaped fused q/k/v, norm and rotation of 2 x 24 heads of 128, M=4608", "fmt": FMT, "linear_ms": c.graph_ms(c.run),
+                          "linear_qkv_ms": c.graph_ms(fused), "qk_norm_rope_ms": c.graph_ms(lambda: dq.dirotq_qk_norm_rope(c.y, qk, q, k))}), flush=True)
+        assert dq.dirotq_workspace_status(c.ws) == 0
+        c.close()
     if "5" in todo:
         M = 4608
         shapes = {"qkv": (3072, 9216), "out": (3072, 3072), "mlp_up": (3072, 12288), "mlp_down": (12288, 3072),

@@ -303,9 +303,10 @@ def test_captured_graph_another_stream_and_two_workspaces():
     assert dq.dirotq_workspace_status(spaces[0]) == 0
 
 
-def test_weights_quantized_right_before_the_call():
+@pytest.mark.parametrize("M", [4, 40, 300])
+def test_weights_quantized_right_before_the_call(M):
     """The product's weights come from the kernel just before the activations' quantizer: nothing of them is read too early."""
-    M, N, K = 4, 4096, 2048
+    N, K = 4096, 2048
     ws = dq.alloc_mxfp4_workspace(M, K)
     x = _data(M, K, 1, torch.bfloat16).cuda()
     w = dq.dirotq_mxfp4_alloc(N, K)
@@ -322,6 +323,56 @@ def test_weights_quantized_right_before_the_call():
         dq.dirotq_mxfp4_quantize(weights[i & 1], out=w)
         dq.dirotq_mxfp4_linear(x, w, y, ws)
         assert torch.equal(y, want[i & 1]), i
+
+
+@pytest.mark.parametrize("layout", [dq.LAYOUT_NK, dq.LAYOUT_KN])
+def test_rows_beyond_32_bits(layout):
+    """Rows so far apart that the last one starts more than 2^31 elements (2^32 bytes) behind the first."""
+    apart, n, w = 2 ** 27 + 16, 20, 64
+    x = torch.empty(19 * apart + w, dtype=torch.bfloat16, device="cuda").as_strided((n, w), (apart, 1))
+    data = _data(n, w, 1, torch.bfloat16)
+    x.copy_(data)
+    t = dq.dirotq_mxfp4_quantize(x, layout=layout)
+    as_rows = data if layout == dq.LAYOUT_NK else data.T.contiguous()
+    codes, scales = _check_quantized(t, as_rows, ref.FLOOR)
+    if layout == dq.LAYOUT_NK:
+        dq.dirotq_mxfp4_dequantize(t, x)
+        assert torch.equal(x.cpu(), ref.values(codes, scales).to(torch.bfloat16))
+        b, bv = _operand(48, w, 5, 3)
+        want, mass = ref.product(ref.values(codes, scales).cuda(), bv)
+        dq.dirotq_mxfp4_gemm(t, b, x[:, :48], dq.alloc_mxfp4_workspace(n, w))
+        _close(x[:, :48], want, mass, w)
+
+
+@pytest.mark.parametrize("M", [2, 60])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_linear_of_infinities_and_nan(M, dtype):
+    """A NaN block of the activations reaches its own row only, whichever kernel quantizes it."""
+    K, N = 300, 70
+    x = _data(M, K, 1, DTYPES[dtype])
+    x[1, 299] = float("inf")
+    x[0, 5] = float("-inf") if M > 2 else x[0, 5]
+    w = dq.dirotq_mxfp4_quantize(_data(N, K, 2).cuda())
+    y = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    dq.dirotq_mxfp4_linear(x.cuda(), w, y, dq.alloc_mxfp4_workspace(M, K))
+    bad = ~torch.isfinite(x).all(1).cuda()
+    assert bool(torch.isnan(y[bad]).all()) and bool(torch.isfinite(y[~bad]).all())
+
+
+def test_an_operand_times_itself_and_a_reused_handle():
+    K = 300
+    a, av = _operand(200, K, 1, 2)
+    ws = dq.alloc_mxfp4_workspace(200, K)
+    y = torch.empty((200, 200), dtype=torch.bfloat16, device="cuda")
+    dq.dirotq_mxfp4_gemm(a, a, y, ws)
+    want, mass = ref.product(av, av)
+    _close(y, want, mass, K)
+    x = _data(200, K, 9)
+    dq.dirotq_mxfp4_quantize(x.cuda(), out=a)
+    v = ref.values(*ref.quantize(x)).cuda()
+    dq.dirotq_mxfp4_gemm(a, a, y, ws)
+    want, mass = ref.product(v, v)
+    _close(y, want, mass, K)
 
 
 def test_refusals_with_handles():

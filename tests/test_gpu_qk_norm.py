@@ -194,6 +194,22 @@ def test_mxfp4_qkv(M, K, hq, hk, D, style, dtype):
     assert bool((y[:, s.width:] == 7).all())
 
 
+@pytest.mark.parametrize("M,D,pad", [(3, 64, 5), (140, 64, 3), (9, 128, 1), (150, 128, 7)])
+def test_mxfp4_qkv_rows_of_any_alignment(M, D, pad):
+    """Rows of y that no wide store can address, and tables with rows of their own: the same bits as aligned ones."""
+    s = Setup(M, 3, 2, D, D, "pairs", torch.float16, M)
+    g = torch.Generator().manual_seed(5)
+    x, w = torch.randn((M, 200), generator=g).half().cuda(), dq.dirotq_mxfp4_quantize((torch.randn((s.width, 200), generator=g) * 0.1).cuda())
+    ws = dq.alloc_mxfp4_workspace(M, 200)
+    wide = torch.empty((2, len(s.cos), D // 2 + 3), device="cuda")
+    wide[0, :, :D // 2], wide[1, :, :D // 2] = s.cos, s.sin
+    plan = dq.QkNorm(3, 2, D, q_weight=s.wq, k_weight=s.wk, rope="pairs", cos=wide[0, :, :D // 2], sin=wide[1, :, :D // 2], positions=s.positions)
+    y, z = torch.empty((M, s.width), dtype=s.dtype, device="cuda"), torch.full((M, s.width + pad), 7, dtype=s.dtype, device="cuda")
+    dq.dirotq_mxfp4_qkv(x, w, y, ws, s.plan)
+    dq.dirotq_mxfp4_qkv(x, w, z[:, :s.width], ws, plan)
+    assert torch.equal(y, z[:, :s.width]) and bool((z[:, s.width:] == 7).all())
+
+
 @pytest.mark.parametrize("M", [40, 200])
 def test_mxfp4_qkv_padding_tokens(M):
     s = Setup(M, 4, 2, 64, 64, "pairs", torch.bfloat16, 1)
