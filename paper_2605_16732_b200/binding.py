@@ -678,14 +678,15 @@ def dirotq_workspace_export_w4a8(layer: Layer, M: int, workspace: torch.Tensor, 
 
 # ------------------------------------------------------------------ MXFP4
 
+_OTHER_DEVICE = "tensors and operands must be on one device"
 _DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
 
 
 def _row_stride(t: torch.Tensor, width: int) -> int:
-    """Elements between the rows of a 2-D cuda tensor whose rows are contiguous.  A single row's stride says nothing: one that would keep the
+    """Elements between the rows of a 2-D tensor whose rows are contiguous.  A single row's stride says nothing: one that would keep the
     library from wide accesses, or is shorter than the row, is replaced."""
     s0, s1 = t.stride()
-    assert t.is_cuda and (s1 == 1 or t.shape[1] == 1), "rows of a cuda tensor must be contiguous"
+    assert s1 == 1 or t.shape[1] == 1, "rows must be contiguous"
     if (s0 >= width and s0 % 8 == 0) or t.shape[0] > 1:
         return s0
     return (max(width, t.shape[1]) + 7) // 8 * 8
@@ -697,6 +698,7 @@ class Mxfp4:
     def __init__(self, handle: int, buffer: torch.Tensor, rows: int, K: int):
         self.handle, self.buffer = handle, buffer
         self.rows, self.K = rows, K
+        self.device = buffer.get_device()  # (the library checks that it is the current one)
 
     def close(self):
         if self.handle:
@@ -719,6 +721,7 @@ def dirotq_mxfp4_bytes(rows: int, K: int) -> int:
 def dirotq_mxfp4_alloc(rows: int, K: int, device="cuda") -> Mxfp4:
     """An operand with a buffer of its own; its contents are undefined until it is quantized or imported."""
     buffer = _alloc_bytes(dirotq_mxfp4_bytes(rows, K), device)
+    assert buffer.get_device() == torch.cuda.current_device(), "operands are made on the current device"
     handle = ctypes.c_void_p(0)
     _check(lib().dirotq_mxfp4_create(rows, K, buffer.data_ptr(), buffer.numel(), ctypes.byref(handle)), "dirotq_mxfp4_create")
     return Mxfp4(handle.value, buffer, rows, K)
@@ -731,6 +734,7 @@ def dirotq_mxfp4_quantize(x: torch.Tensor, out: Mxfp4 | None = None, scale_rule:
     if out is None:
         out = dirotq_mxfp4_alloc(rows, K, x.device)
     assert out.rows == rows and out.K == K, "the operand has another shape"
+    assert x.get_device() == out.device, _OTHER_DEVICE
     st = (_lib or lib()).dirotq_mxfp4_quantize(x.data_ptr(), _DTYPES[x.dtype], layout, _row_stride(x, K if layout == LAYOUT_NK else rows), scale_rule,
                                                out.handle, _stream(stream))
     if st:
@@ -740,6 +744,7 @@ def dirotq_mxfp4_quantize(x: torch.Tensor, out: Mxfp4 | None = None, scale_rule:
 
 def dirotq_mxfp4_dequantize(t: Mxfp4, y: torch.Tensor, stream=None) -> None:
     assert y.shape == (t.rows, t.K)
+    assert y.get_device() == t.device, _OTHER_DEVICE
     st = (_lib or lib()).dirotq_mxfp4_dequantize(t.handle, y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, t.K), _stream(stream))
     if st:
         _check(st, "dirotq_mxfp4_dequantize")
@@ -753,6 +758,7 @@ def dirotq_mxfp4_import(codes: torch.Tensor, scales: torch.Tensor, K: int, out: 
     if out is None:
         out = dirotq_mxfp4_alloc(rows, K, codes.device)
     assert (out.rows, out.K) == (rows, K), "the operand has another shape"
+    assert codes.get_device() == scales.get_device() == out.device, _OTHER_DEVICE
     _check(lib().dirotq_mxfp4_import(codes.data_ptr(), scales.data_ptr(), out.handle, _stream(stream)), "dirotq_mxfp4_import")
     return out
 
@@ -774,7 +780,7 @@ def alloc_mxfp4_workspace(M: int, K: int, device="cuda") -> torch.Tensor:
 def _bias_ptr(bias, y, N):
     if bias is None:
         return None
-    assert bias.is_cuda and bias.is_contiguous() and bias.dtype == y.dtype and bias.numel() == N
+    assert bias.get_device() == y.get_device() and bias.is_contiguous() and bias.dtype == y.dtype and bias.numel() == N
     return bias.data_ptr()
 
 
@@ -782,6 +788,7 @@ def dirotq_mxfp4_gemm(a: Mxfp4, b: Mxfp4, y: torch.Tensor, workspace: torch.Tens
     """y [a.rows, b.rows] (bf16 or f16, rows of any stride) = a b^T + bias."""
     N = b.rows
     assert y.shape == (a.rows, N)
+    assert y.get_device() == workspace.get_device() == a.device == b.device, _OTHER_DEVICE
     st = (_lib or lib()).dirotq_mxfp4_gemm(a.handle, b.handle, _bias_ptr(bias, y, N), y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, N),
                                            workspace.data_ptr(), workspace.numel(), _stream(stream))
     if st:
@@ -794,6 +801,7 @@ def dirotq_mxfp4_linear(x: torch.Tensor, w: Mxfp4, y: torch.Tensor, workspace: t
     M, K = x.shape
     N = w.rows
     assert K == w.K and y.shape == (M, N)
+    assert x.get_device() == y.get_device() == workspace.get_device() == w.device, _OTHER_DEVICE
     st = (_lib or lib()).dirotq_mxfp4_linear(x.data_ptr(), _DTYPES[x.dtype], _row_stride(x, K), M, scale_rule, w.handle, _bias_ptr(bias, y, N),
                                              y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, N), workspace.data_ptr(), workspace.numel(), _stream(stream))
     if st:
@@ -848,19 +856,20 @@ def dirotq_qk_norm_rope(x: torch.Tensor, qk: QkNorm, q_out: torch.Tensor, k_out:
     wq, wk = qk._widths
     M, wx = x.shape
     rows, width = k_out.shape
-    dtype = x.dtype
+    dtype, device = x.dtype, x.get_device()
+    assert device == q_out.get_device() == k_out.get_device() == (_current_device or torch.cuda.current_device)(), _OTHER_DEVICE
     assert q_out.shape[0] == M and q_out.shape[1] >= wq and width >= wk and q_out.dtype == dtype and k_out.dtype == dtype
     if v_out is None:
         assert wx >= wq + wk
         v_ptr, ldv = None, 0
     else:
-        assert wx >= wq + 2 * wk and v_out.dtype == dtype and v_out.shape[0] == rows and v_out.shape[1] >= wk
+        assert wx >= wq + 2 * wk and v_out.dtype == dtype and v_out.shape[0] == rows and v_out.shape[1] >= wk and v_out.get_device() == device
         v_ptr, ldv = v_out.data_ptr(), _row_stride(v_out, wk)
     if slots is None:
         assert rows == M
         s_ptr, rows = None, 0
     else:
-        assert slots.is_cuda and slots.is_contiguous() and slots.dtype == torch.int32 and slots.numel() == M
+        assert slots.get_device() == device and slots.is_contiguous() and slots.dtype == torch.int32 and slots.numel() == M
         s_ptr = slots.data_ptr()
     st = (_lib or lib()).dirotq_qk_norm_rope(x.data_ptr(), _DTYPES[dtype], M, _row_stride(x, wx), qk._ref(M), q_out.data_ptr(), _row_stride(q_out, wq),
                                              k_out.data_ptr(), _row_stride(k_out, wk), v_ptr, ldv, s_ptr, rows, _stream(stream))
@@ -880,6 +889,7 @@ def dirotq_mxfp4_qkv(x: torch.Tensor, w: Mxfp4, y: torch.Tensor, workspace: torc
     M, K = x.shape
     N = w.rows
     assert K == w.K and y.shape == (M, N)
+    assert x.get_device() == y.get_device() == workspace.get_device() == w.device, _OTHER_DEVICE
     st = (_lib or lib()).dirotq_mxfp4_qkv(x.data_ptr(), _DTYPES[x.dtype], _row_stride(x, K), M, scale_rule, w.handle, _bias_ptr(bias, y, N), qk._ref(M),
                                           y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, N), workspace.data_ptr(), workspace.numel(), _stream(stream))
     if st:
