@@ -179,7 +179,7 @@ DIROTQ_API dirotq_status_t dirotq_int_gemm_debug(const int8_t* act_codes, int M,
                                       int32_t* partials, void* workspace, size_t workspace_bytes,
                                       dirotq_stream_t stream);
 
-/* Tuning knob of the second kernels (all four formats): output columns per tile.
+/* Tuning knob of the second kernels (all four formats) and of the MXFP4 products: output columns per tile.
  * 0 (default): chosen per call from M, N and the number of SMs, the shortest schedule of the plans below, 66 apart (NVFP4: 256
  * columns unless 128-column tiles, at 0.6 of a wide one, shorten the schedule);
  * 128 or 256: forced; 64: the grouped INT4 kernel's plan for few token rows, forced, one CTA per tile (32: the same with half the
@@ -192,7 +192,8 @@ DIROTQ_API dirotq_status_t dirotq_int_gemm_debug(const int8_t* act_codes, int M,
  * each CTA loading its own rows and one half of the weight tile); 192: the grouped INT4 kernel's plan
  * with three epilogue warpgroups (64 columns per thread); 512: the NVFP4 kernel in pairs of CTAs (as 258), forced;
  * 0 takes it where its schedule is the shortest (every FLUX
- * shape at M = 4608); for W4A8 128 is single CTAs, 256 and 512 are CTA pairs with 128 and 256 columns.  A value that names a plan of
+ * shape at M = 4608); for W4A8 128 is single CTAs, 256 and 512 are CTA pairs with 128 and 256 columns; for the MXFP4 products 64 and 128
+ * are single CTAs with that many columns (64 not where a head of 128 columns is normed in the product), 512 CTA pairs with 256.  A value that names a plan of
  * one kernel leaves the other formats' kernels choosing for themselves.  Process-wide; results do not depend on it, 66
  * apart (each output element is accumulated in the same order).  Other values: DIROTQ_ERR_INVALID_ARG. */
 DIROTQ_API dirotq_status_t dirotq_set_gemm_tile(int columns);

@@ -3,6 +3,10 @@
 // Memory sets the time: 4 bytes a value in 16 bits, and the tables.  head_dim / 8 lanes hold a head, eight consecutive elements each, so a warp
 // holds 32 / (head_dim / 8) whole heads side by side in memory; it takes kHeads such sets of one token's q, k or v at once, their loads in
 // flight together, with the token's cosines and sines kept in registers for all of them.  The sum of squares is a few shuffles.
+//
+// Measured (bf16, q, k and v copied): 4608 tokens, 3 x 24 heads of 128, 30.7 us, 5.5 TB/s; 18432 tokens 6.1 TB/s; heads of 64 15.0 us; 64 tokens of 32 + 2 x 8
+// heads 3.0 us (latency).  4173 tokens, 3 x 16 heads of 72 in fp16, half of each turned: 15 us, 3.9 TB/s: instructions (27 of 32 lanes hold
+// heads, and a sum over nine lanes is four steps of shuffle and test).  (One block of threads per token, weights and angles per head from memory: 67 us for the first.)
 #include "mxfp4.cuh"
 #include "ptx.cuh"
 
