@@ -712,6 +712,15 @@ class Mxfp4:
             pass
 
 
+def _made_for(stream, *tensors) -> None:
+    """These were allocated on the current stream just now and are written on `stream`: it comes after what the current stream may still do with
+    their memory, and the allocator knows of it."""
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+        for t in tensors:
+            t.record_stream(stream)
+
+
 def dirotq_mxfp4_bytes(rows: int, K: int) -> int:
     out = ctypes.c_size_t(0)
     _check(lib().dirotq_mxfp4_bytes(rows, K, ctypes.byref(out)), "dirotq_mxfp4_bytes")
@@ -733,6 +742,7 @@ def dirotq_mxfp4_quantize(x: torch.Tensor, out: Mxfp4 | None = None, scale_rule:
     rows, K = x.shape if layout == LAYOUT_NK else (x.shape[1], x.shape[0])
     if out is None:
         out = dirotq_mxfp4_alloc(rows, K, x.device)
+        _made_for(stream, out.buffer)
     assert out.rows == rows and out.K == K, "the operand has another shape"
     assert x.get_device() == out.device, _OTHER_DEVICE
     st = (_lib or lib()).dirotq_mxfp4_quantize(x.data_ptr(), _DTYPES[x.dtype], layout, _row_stride(x, K if layout == LAYOUT_NK else rows), scale_rule,
@@ -757,6 +767,7 @@ def dirotq_mxfp4_import(codes: torch.Tensor, scales: torch.Tensor, K: int, out: 
     assert scales.is_cuda and scales.is_contiguous() and scales.dtype == torch.uint8 and tuple(scales.shape) == (rows, -(-K // 32))
     if out is None:
         out = dirotq_mxfp4_alloc(rows, K, codes.device)
+        _made_for(stream, out.buffer)
     assert (out.rows, out.K) == (rows, K), "the operand has another shape"
     assert codes.get_device() == scales.get_device() == out.device, _OTHER_DEVICE
     _check(lib().dirotq_mxfp4_import(codes.data_ptr(), scales.data_ptr(), out.handle, _stream(stream)), "dirotq_mxfp4_import")
@@ -766,6 +777,7 @@ def dirotq_mxfp4_import(codes: torch.Tensor, scales: torch.Tensor, K: int, out: 
 def dirotq_mxfp4_export(t: Mxfp4, stream=None):
     codes = torch.empty((t.rows, -(-t.K // 2)), dtype=torch.uint8, device=t.buffer.device)
     scales = torch.empty((t.rows, -(-t.K // 32)), dtype=torch.uint8, device=t.buffer.device)
+    _made_for(stream, codes, scales)
     _check(lib().dirotq_mxfp4_export(t.handle, codes.data_ptr(), scales.data_ptr(), _stream(stream)), "dirotq_mxfp4_export")
     return codes, scales
 

@@ -303,6 +303,27 @@ def test_captured_graph_another_stream_and_two_workspaces():
     assert dq.dirotq_workspace_status(spaces[0]) == 0
 
 
+def test_operands_made_on_another_stream():
+    """Memory that the current stream is still to write is handed out again: an operand made in it on another stream comes after."""
+    rows, K = 300, 4096
+    x = _data(rows, K, 1, torch.bfloat16).cuda()
+    codes, scales = ref.quantize(x.cpu())
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for make in (lambda: dq.dirotq_mxfp4_quantize(x, stream=side), lambda: dq.dirotq_mxfp4_import(ref.pack(codes).cuda(), scales.cuda(), K, stream=side)):
+        old = dq.dirotq_mxfp4_alloc(rows, K)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        old.buffer.fill_(255)
+        where = old.buffer.data_ptr()
+        old.close()
+        del old
+        t = make()
+        torch.cuda.synchronize()
+        got, got_scales = dq.dirotq_mxfp4_export(t)
+        assert torch.equal(ref.unpack(got.cpu(), K), codes) and torch.equal(got_scales.cpu(), scales), where == t.buffer.data_ptr()
+
+
 @pytest.mark.parametrize("M", [4, 40, 300])
 def test_weights_quantized_right_before_the_call(M):
     """The product's weights come from the kernel just before the activations' quantizer: nothing of them is read too early."""
