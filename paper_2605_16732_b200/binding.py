@@ -686,8 +686,10 @@ def _row_stride(t: torch.Tensor, width: int) -> int:
     """Elements between the rows of a 2-D tensor whose rows are contiguous.  A single row's stride says nothing: one that would keep the
     library from wide accesses, or is shorter than the row, is replaced."""
     s0, s1 = t.stride()
+    if s1 == 1 and s0 >= width and not s0 & 7:
+        return s0
     assert s1 == 1 or t.shape[1] == 1, "rows must be contiguous"
-    if (s0 >= width and s0 % 8 == 0) or t.shape[0] > 1:
+    if t.shape[0] > 1:
         return s0
     return (max(width, t.shape[1]) + 7) // 8 * 8
 
@@ -867,24 +869,25 @@ def dirotq_qk_norm_rope(x: torch.Tensor, qk: QkNorm, q_out: torch.Tensor, k_out:
     """x [M, (heads_q + 2 heads_kv) head_dim]; q_out [M, heads_q head_dim]; k_out, v_out [M or slots, heads_kv head_dim]; slots: cuda int32 [M]."""
     wq, wk = qk._widths
     M, wx = x.shape
-    rows, width = k_out.shape
+    mq, nq = q_out.shape
+    rows, nk = k_out.shape
     dtype, device = x.dtype, x.get_device()
+    assert mq == M and nq >= wq and nk >= wk and wx >= (wq + wk if v_out is None else wq + 2 * wk)
+    assert q_out.dtype is dtype and k_out.dtype is dtype
     assert device == q_out.get_device() == k_out.get_device() == (_current_device or torch.cuda.current_device)(), _OTHER_DEVICE
-    assert q_out.shape[0] == M and q_out.shape[1] >= wq and width >= wk and q_out.dtype == dtype and k_out.dtype == dtype
-    if v_out is None:
-        assert wx >= wq + wk
-        v_ptr, ldv = None, 0
-    else:
-        assert wx >= wq + 2 * wk and v_out.dtype == dtype and v_out.shape[0] == rows and v_out.shape[1] >= wk and v_out.get_device() == device
+    ldx, ldq, ldk = _row_stride(x, wx), _row_stride(q_out, wq), _row_stride(k_out, wk)
+    v_ptr = s_ptr = None
+    ldv = num_slots = 0
+    if v_out is not None:
+        assert v_out.dtype is dtype and v_out.shape[0] == rows and v_out.shape[1] >= wk and v_out.get_device() == device
         v_ptr, ldv = v_out.data_ptr(), _row_stride(v_out, wk)
     if slots is None:
         assert rows == M
-        s_ptr, rows = None, 0
     else:
-        assert slots.get_device() == device and slots.is_contiguous() and slots.dtype == torch.int32 and slots.numel() == M
-        s_ptr = slots.data_ptr()
-    st = (_lib or lib()).dirotq_qk_norm_rope(x.data_ptr(), _DTYPES[dtype], M, _row_stride(x, wx), qk._ref(M), q_out.data_ptr(), _row_stride(q_out, wq),
-                                             k_out.data_ptr(), _row_stride(k_out, wk), v_ptr, ldv, s_ptr, rows, _stream(stream))
+        assert slots.get_device() == device and slots.is_contiguous() and slots.dtype is torch.int32 and slots.numel() == M
+        s_ptr, num_slots = slots.data_ptr(), rows
+    st = (_lib or lib()).dirotq_qk_norm_rope(x.data_ptr(), _DTYPES[dtype], M, ldx, qk._ref(M), q_out.data_ptr(), ldq, k_out.data_ptr(), ldk, v_ptr, ldv,
+                                             s_ptr, num_slots, _stream(stream))
     if st:
         _check(st, "dirotq_qk_norm_rope")
 
