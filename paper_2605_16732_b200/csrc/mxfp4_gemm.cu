@@ -83,7 +83,7 @@ struct MxKernelParams {
     uint8_t* y;
     long long ldy;
     int* status;
-    int wide_out;          // rows of y are 16-byte aligned
+    int wide_out;          // rows of y are 16-byte (1) or 32-byte (2) aligned
     int early;             // b may be read while the previous kernel runs
     // norm and rotation of q and k
     int q_cols, k_end;     // columns [0, q_cols) are q, [q_cols, k_end) are k
@@ -96,7 +96,7 @@ struct MxKernelParams {
     const float* cos_table;
     const float* sin_table;
     long long ld_table;
-    int wide_table;        // rows of both tables are 16-byte aligned
+    int wide_table;        // rows of both tables are 32-byte aligned
     int num_positions;
     const int32_t* positions;
     // FUSE: the activations as they are
@@ -241,15 +241,42 @@ __device__ __forceinline__ void store_run(const MxKernelParams& p, int row0, int
             if (r < rows) y[r * p.ldy + lane] = e[r];
 }
 
-// Cosines and sines of four consecutive angles (`wide`: 16-byte aligned).
-__device__ __forceinline__ void load_angles(const float* cs, const float* sn, int wide, float (&c)[4], float (&s)[4]) {
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(lo), "r"(hi));
+    return v;
+}
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) { return pair_of(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ void split_pair(uint64_t v, uint32_t& lo, uint32_t& hi) { asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+
+// Cosines and sines of eight consecutive angles (`wide`: 32-byte aligned, one load each).
+__device__ __forceinline__ void load_angles(const float* cs, const float* sn, int wide, float (&c)[8], float (&s)[8]) {
     if (wide) {
-        const float4 a = __ldg(reinterpret_cast<const float4*>(cs)), b = __ldg(reinterpret_cast<const float4*>(sn));
-        c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w;
-        s[0] = b.x; s[1] = b.y; s[2] = b.z; s[3] = b.w;
+        asm volatile("ld.global.nc.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]), "=f"(c[4]), "=f"(c[5]), "=f"(c[6]), "=f"(c[7])
+                     : "l"(cs));
+        asm volatile("ld.global.nc.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(s[0]), "=f"(s[1]), "=f"(s[2]), "=f"(s[3]), "=f"(s[4]), "=f"(s[5]), "=f"(s[6]), "=f"(s[7])
+                     : "l"(sn));
     } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 8; ++k) {
             c[k] = __ldg(cs + k);
             s[k] = __ldg(sn + k);
         }
@@ -257,118 +284,168 @@ __device__ __forceinline__ void load_angles(const float* cs, const float* sn, in
 }
 
 // The columns of a fused projection's tile that one warp has: two runs of 32 columns, at `run0` and `run1` of the group's, of SETS * 16 rows from
-// row0.  Runs are halves of one head: of 64 columns (run1 = run0 + 32), or of 128, whose other halves are another warp's (run1 = run0 + 64: element
-// i and i + D/2 are always in one warp); those two warps add up their sums of squares through s_sum, `pair_bar` their named barrier.
-//
-// raw[set][run][4 k + 2 hi + e] is column 8 k + 2 t + e of row 16 set + 8 hi + l / 4 as it is loaded, and, exchanged within the row's four lanes,
-// column 8 t + 2 k + e.
-template <int SETS, bool F16>
-__device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], const MxKernelParams& p, int row0, int n0, int run0, int run1, int lane, const float* s_b,
-                                            const float* s_hw, float* s_sum, const float* s_sum_other, int pair_bar, uint32_t edge, bool whole) {
+// row0.  raw[set][run][4 k + 2 hi + e] is column 8 k + 2 t + e of the run, row 16 set + 8 hi + l / 4, and is so through bias, sum of squares and
+// norm; then the row's four lanes exchange it, so that each has whole sectors of the tables and of y (the bound here is the number of lines that
+// loads and stores touch: a row per lane, with half the instructions but 32 lines a load, took 79 us where this takes 7x).
+//   HALVES: element i and i + D/2 are in one warp: the runs are the halves of a head of 64 (run1 = run0 + 32), or halves of the halves of one of
+//           128 (run1 = run0 + 64); a lane has columns 8 t .. 8 t + 7 of both runs, which are turned with one another by eight angles.
+//   else:   64 columns side by side; a lane has columns 16 t .. 16 t + 15, eight pairs.
+// The two warps of a head of 128 (`split`) add up their sums of squares through s_sum, `pair_bar` their named barrier.
+template <int SETS, bool F16, bool HALVES>
+__device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], const MxKernelParams& p, int row0, int n0, int run0, int run1, bool split, int lane,
+                                            const float* s_b, const float* s_hw, float* s_sum, const float* s_sum_other, int pair_bar, uint32_t edge, bool whole) {
     const int t = lane & 3, r4 = lane >> 2;
     const bool head = n0 + run0 < p.k_end;  // q or k (the same for the whole warp, and for the two of a head)
-    float ss[SETS][2];
+    const int at0 = run0 & ((1 << p.head_shift) - 1), at1 = run1 & ((1 << p.head_shift) - 1);  // the runs' places in the head
+    uint64_t sum[SETS][2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 b = *reinterpret_cast<const float2*>(s_b + (j ? run1 : run0) + 8 * k + 2 * t);
+            const uint64_t b2 = pair_of(b.x, b.y);
+#pragma unroll
+            for (int set = 0; set < SETS; ++set)
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) {
+                    uint32_t &x = raw[set][j][4 * k + 2 * hi], &y = raw[set][j][4 * k + 2 * hi + 1];
+                    const uint64_t v = add2(pair_of(x, y), b2);
+                    sum[set][hi] = j + k ? fma2(v, v, sum[set][hi]) : mul2(v, v);
+                    split_pair(v, x, y);
+                }
+        }
+    int pos[SETS][2];
+    bool turned[SETS][2], all = true;
 #pragma unroll
     for (int set = 0; set < SETS; ++set)
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t even[4], odd[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    even[k] = raw[set][j][4 * k + 2 * hi];
-                    odd[k] = raw[set][j][4 * k + 2 * hi + 1];
-                }
-                transpose4(even, t);
-                transpose4(odd, t);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 b = *reinterpret_cast<const float2*>(s_b + (j ? run1 : run0) + 8 * t + 2 * k);
-                    const float x = __uint_as_float(even[k]) + b.x, y = __uint_as_float(odd[k]) + b.y;
-                    sum = fmaf(x, x, fmaf(y, y, sum));
-                    raw[set][j][4 * k + 2 * hi] = __float_as_uint(x);
-                    raw[set][j][4 * k + 2 * hi + 1] = __float_as_uint(y);
-                }
-            }
-            ss[set][hi] = sum;
+            const int row = row0 + 16 * set + 8 * hi + r4;
+            const bool here = head && row < p.M;
+            pos[set][hi] = row;
+            if (here && p.positions != nullptr) pos[set][hi] = __ldg(p.positions + row);
+            turned[set][hi] = here && (p.rope == DIROTQ_ROPE_NONE || (pos[set][hi] >= 0 && pos[set][hi] < p.num_positions));
+            all = all && (turned[set][hi] || !here);
         }
+    // A set's angles are on their way while the rows before it are packed and stored, the first's during the norm (row 0's where a row is not turned).
+    float c[8], s[8];
+    auto fetch = [&](int set, int hi) {
+        if (!head || p.rope == DIROTQ_ROPE_NONE) return;
+        const long long a = static_cast<long long>(turned[set][hi] ? pos[set][hi] : 0) * p.ld_table + (HALVES ? at0 : at0 >> 1) + 8 * t;
+        load_angles(p.cos_table + a, p.sin_table + a, p.wide_table, c, s);
+    };
+
     if (head && p.norm) {
+        float ss[SETS][2];
 #pragma unroll
         for (int set = 0; set < SETS; ++set)
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) {
+                uint32_t x, y;
+                split_pair(sum[set][hi], x, y);
+                ss[set][hi] = __uint_as_float(x) + __uint_as_float(y);
                 ss[set][hi] += __shfl_xor_sync(0xffffffffu, ss[set][hi], 1);
                 ss[set][hi] += __shfl_xor_sync(0xffffffffu, ss[set][hi], 2);
-                if (run1 != run0 + 32 && t == 0) s_sum[16 * set + 8 * hi + r4] = ss[set][hi];
+                if (split && t == 0) s_sum[16 * set + 8 * hi + r4] = ss[set][hi];
             }
-        if (run1 != run0 + 32) {
+        if (split) {
             asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
 #pragma unroll
             for (int set = 0; set < SETS; ++set)
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) ss[set][hi] += s_sum_other[16 * set + 8 * hi + r4];
         }
+#pragma unroll
+        for (int set = 0; set < SETS; ++set)
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) ss[set][hi] = rsqrtf(ss[set][hi] * p.inv_dim + p.eps);
+        const float* w = s_hw + (n0 + run0 < p.q_cols ? 0 : 128);
+        auto scale = [&](bool every) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 g = *reinterpret_cast<const float2*>(w + (j ? at1 : at0) + 8 * k + 2 * t);
+#pragma unroll
+                    for (int set = 0; set < SETS; ++set)
+#pragma unroll
+                        for (int hi = 0; hi < 2; ++hi) {
+                            uint32_t &x = raw[set][j][4 * k + 2 * hi], &y = raw[set][j][4 * k + 2 * hi + 1];
+                            const uint64_t v = mul2(pair_of(x, y), mul2(pair_of(g.x, g.y), pair_of(ss[set][hi], ss[set][hi])));
+                            if (every || turned[set][hi]) split_pair(v, x, y);
+                        }
+                }
+        };
+        if (__all_sync(0xffffffffu, all)) scale(true);
+        else scale(false);
     }
-    const float* w = s_hw + (n0 + run0 < p.q_cols ? 0 : 128);
-    const int at0 = run0 & ((1 << p.head_shift) - 1), at1 = run1 & ((1 << p.head_shift) - 1);  // the runs' places in the head
+    fetch(0, 0);
 #pragma unroll
     for (int set = 0; set < SETS; ++set)
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
             const int row = row0 + 16 * set + 8 * hi + r4;
-            int pos = row;
-            if (head && p.positions != nullptr && row < p.M) pos = __ldg(p.positions + row);
-            if (head && row < p.M && (p.rope == DIROTQ_ROPE_NONE || (pos >= 0 && pos < p.num_positions))) {
-                auto v = [&](int j, int e) -> uint32_t& { return raw[set][j][4 * (e >> 1) + 2 * hi + (e & 1)]; };
-                if (p.norm) {
-                    const float r = rsqrtf(ss[set][hi] * p.inv_dim + p.eps);
+            // the row's values as this lane has them from here on: HALVES: run0's columns 8 t .., then run1's; else columns 16 t ..
+            uint32_t v[16];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < 2; ++j) {
+                uint32_t even[4], odd[4];
 #pragma unroll
-                        for (int e = 0; e < 8; e += 4) {
-                            const float4 g = *reinterpret_cast<const float4*>(w + (j ? at1 : at0) + 8 * t + e);
-                            v(j, e) = __float_as_uint(__uint_as_float(v(j, e)) * (r * g.x));
-                            v(j, e + 1) = __float_as_uint(__uint_as_float(v(j, e + 1)) * (r * g.y));
-                            v(j, e + 2) = __float_as_uint(__uint_as_float(v(j, e + 2)) * (r * g.z));
-                            v(j, e + 3) = __float_as_uint(__uint_as_float(v(j, e + 3)) * (r * g.w));
-                        }
+                for (int k = 0; k < 4; ++k) {
+                    const int J = HALVES ? 4 * j + k : 2 * k + j;  // columns 8 J + 2 t, + 1 of the 64
+                    even[k] = raw[set][J >> 2][4 * (J & 3) + 2 * hi];
+                    odd[k] = raw[set][J >> 2][4 * (J & 3) + 2 * hi + 1];
                 }
-                const long long table = static_cast<long long>(pos) * p.ld_table;
-                auto turn = [&](uint32_t& x, uint32_t& y, float c, float s) {
-                    const float a = __uint_as_float(x), b = __uint_as_float(y);
-                    x = __float_as_uint(a * c - b * s);
-                    y = __float_as_uint(a * s + b * c);
-                };
-                if (p.rope == DIROTQ_ROPE_PAIRS) {
+                transpose4(even, t);
+                transpose4(odd, t);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        float c[4], s[4];
-                        const int a = ((j ? at1 : at0) >> 1) + 4 * t;
-                        load_angles(p.cos_table + table + a, p.sin_table + table + a, p.wide_table, c, s);
+                for (int k = 0; k < 4; ++k) {
+                    v[8 * j + 2 * k] = even[k];
+                    v[8 * j + 2 * k + 1] = odd[k];
+                }
+            }
+            if (p.rope != DIROTQ_ROPE_NONE && turned[set][hi]) {
+                if constexpr (HALVES) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) turn(v(j, 2 * k), v(j, 2 * k + 1), c[k], s[k]);
+                    for (int k = 0; k < 8; k += 2) {
+                        const uint64_t x = pair_of(v[k], v[k + 1]), y = pair_of(v[8 + k], v[9 + k]), cc = pair_of(c[k], c[k + 1]);
+                        split_pair(fma2(x, cc, mul2(y, pair_of(-s[k], -s[k + 1]))), v[k], v[k + 1]);
+                        split_pair(fma2(y, cc, mul2(x, pair_of(s[k], s[k + 1]))), v[8 + k], v[9 + k]);
                     }
-                } else if (p.rope == DIROTQ_ROPE_HALVES) {
+                } else {
 #pragma unroll
-                    for (int e = 0; e < 8; e += 4) {
-                        float c[4], s[4];
-                        const int a = at0 + 8 * t + e;
-                        load_angles(p.cos_table + table + a, p.sin_table + table + a, p.wide_table, c, s);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) turn(v(0, e + k), v(1, e + k), c[k], s[k]);
+                    for (int k = 0; k < 8; ++k) {
+                        const float x = __uint_as_float(v[2 * k]), y = __uint_as_float(v[2 * k + 1]);
+                        v[2 * k] = __float_as_uint(x * c[k] - y * s[k]);
+                        v[2 * k + 1] = __float_as_uint(x * s[k] + y * c[k]);
                     }
                 }
             }
+            if (2 * set + hi + 1 < 2 * SETS) fetch(set + hi, hi ^ 1);
+            uint32_t o[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = pack2<F16>(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
             const int rows = min(8, p.M - row0 - 16 * set - 8 * hi);  // (none or less where the tile ends before)
+            if constexpr (HALVES) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t o[4];
+                for (int j = 0; j < 2; ++j)
+                    store_run(p, row - r4, rows, n0 + (j ? run1 : run0), lane, make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]), edge, whole);
+            } else if (whole && p.wide_out == 2) {
+                if (r4 < rows)
+                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row) * p.ldy + n0 + run0 + 16 * t),
+                                 "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7])
+                                 : "memory");
+            } else {  // (lane t's 16 columns are run t / 2's, from 16 (t % 2): as halves of eight, in the order that store_run has them)
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    o[k] = pack2<F16>(__uint_as_float(raw[set][j][4 * k + 2 * hi]), __uint_as_float(raw[set][j][4 * k + 2 * hi + 1]));
-                store_run(p, row - r4, rows, n0 + (j ? run1 : run0), lane, make_uint4(o[0], o[1], o[2], o[3]), edge, whole);
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t w4[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t first = __shfl_sync(0xffffffffu, o[i], (lane & ~3) + 2 * j + (t >> 1)), other = __shfl_sync(0xffffffffu, o[4 + i], (lane & ~3) + 2 * j + (t >> 1));
+                        w4[i] = t & 1 ? other : first;
+                    }
+                    store_run(p, row - r4, rows, n0 + (j ? run1 : run0), lane, make_uint4(w4[0], w4[1], w4[2], w4[3]), edge, whole);
+                }
             }
         }
 }
@@ -424,12 +501,14 @@ __device__ __forceinline__ void quantize_resident(const MxKernelParams& p, uint3
     }
 }
 
-template <int BN, bool PAIR, bool QKV, bool F16, bool FUSE>
+// HEADS: 0 a product alone, 1 its q and k with norm and rotation of adjacent pairs (or none), 2 of halves (two kernels: one with both branches spills).
+template <int BN, bool PAIR, int HEADS, bool F16, bool FUSE>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ MxKernelParams p) {
     using P = MxPlan<BN, PAIR, FUSE>;
     constexpr int NB = P::NB, STAGES = P::STAGES, ACC_BUFS = P::ACC_BUFS, STAGE_BYTES = P::STAGE_BYTES, KBS = P::KBS;
     constexpr int CW = PAIR ? 128 : BN;  // columns of an epilogue group
+    constexpr bool QKV = HEADS != 0;
     constexpr bool SPLIT_REGS = QKV || CW == 128;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -492,7 +571,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
     // kernel before they do)
 
     if (warp < 4) {
-        if constexpr (SPLIT_REGS) reg_dealloc<56>();  // 128 * 56 + 512 * 104 registers of the 640 * 96 at launch
+        if constexpr (SPLIT_REGS) reg_dealloc<32>();  // 128 * 32 + 512 * 112 registers are the 640 * 96 at launch
         if (warp == 0) {
             // ------------------------------------------------------------ producer
             RingPos<STAGES> at;
@@ -648,7 +727,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
         // Loads of 16 lanes x 256 bits leave lane l with columns 8 J + 2 t, + 1 (t = l % 4) of rows l / 4 and l / 4 + 8: exchanged within the four lanes
         // of a row (transpose4), each lane has runs of 8 consecutive columns, 32 m + 8 t, of its two rows, 64 bytes of a row side by side in a
         // store.  (Through shared memory and TMA stores instead: the same time at K = 12288, and 32 KB that hold a stage of operands here.)
-        if constexpr (SPLIT_REGS) reg_alloc<104>();
+        if constexpr (SPLIT_REGS) reg_alloc<112>();
         constexpr int RUNS = CW / 32, CH = CW / 64;
         const int q = warp & 3, second = ((warp - 4) >> 2) & 1, group = (warp - 4) >> 3, gt = threadIdx.x - 128 - group * GROUP_THREADS;
         constexpr bool HEADS128 = QKV && CW == 128;  // the second warp of a quadrant takes other columns, not rows
@@ -691,8 +770,8 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             };
             if constexpr (QKV) {
                 constexpr int SETS = HEADS128 ? 2 : 1;
-                const bool split = HEADS128 && p.head_shift == 7;
-                const int run0 = HEADS128 ? (split ? 32 : 64) * second : 0, run1 = run0 + (split ? 64 : 32);
+                const bool split = HEADS128 && p.head_shift == 7, apart = split && HEADS == 2;
+                const int run0 = HEADS128 ? (apart ? 32 : 64) * second : 0, run1 = run0 + (apart ? 64 : 32);
                 uint32_t raw[SETS][2][16];
                 if (stored) {
 #pragma unroll
@@ -710,8 +789,8 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
                 hand_back();
                 if (!stored) continue;
                 float* sums = reinterpret_cast<float*>(smem_gen + P::SUM_OFFSET);
-                store_heads<SETS, F16>(raw, p, row0, n0, run0, run1, lane, s_b, s_hw, sums + (warp - 4) * 32, sums + ((warp - 4) ^ 4) * 32,
-                                       3 + group * 4 + q, edge, whole);
+                float *mine = sums + (warp - 4) * 32, *other = sums + ((warp - 4) ^ 4) * 32;
+                store_heads<SETS, F16, HEADS == 2>(raw, p, row0, n0, run0, run1, split, lane, s_b, s_hw, mine, other, 3 + group * 4 + q, edge, whole);
             } else {
                 uint32_t raw[CH][32];  // [columns 64 c ..][4 j + 2 (row + 8) + (column + 1)], J = 8 c + j
                 if (stored) {
@@ -769,10 +848,10 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
     }
 }
 
-template <int BN, bool PAIR, bool QKV, bool F16, bool FUSE>
+template <int BN, bool PAIR, int HEADS, bool F16, bool FUSE>
 dirotq_status_t launch_kernel_of(const MxGemmArgs& a, MxKernelParams& p, cudaStream_t stream) {
     using P = MxPlan<BN, PAIR, FUSE>;
-    auto kern = mx_gemm_kernel<BN, PAIR, QKV, F16, FUSE>;
+    auto kern = mx_gemm_kernel<BN, PAIR, HEADS, F16, FUSE>;
     const int device = a.b->device, sms = sm_count(device);
     static SmemOptIn<1> opt_in;
     if (!opt_in.ensure(kern, 0, device, P::SMEM_BYTES)) return DIROTQ_ERR_CUDA;
@@ -794,11 +873,11 @@ dirotq_status_t launch_kernel_of(const MxGemmArgs& a, MxKernelParams& p, cudaStr
 
 template <int BN, bool PAIR, bool FUSE>
 dirotq_status_t launch_plan(const MxGemmArgs& a, MxKernelParams& p, cudaStream_t stream) {
-    if (a.qk)
-        return a.y_dtype == DIROTQ_DTYPE_F16 ? launch_kernel_of<BN, PAIR, true, true, FUSE>(a, p, stream)
-                                             : launch_kernel_of<BN, PAIR, true, false, FUSE>(a, p, stream);
-    return a.y_dtype == DIROTQ_DTYPE_F16 ? launch_kernel_of<BN, PAIR, false, true, FUSE>(a, p, stream)
-                                         : launch_kernel_of<BN, PAIR, false, false, FUSE>(a, p, stream);
+    const bool f16 = a.y_dtype == DIROTQ_DTYPE_F16;
+    if (a.qk && a.qk->rope == DIROTQ_ROPE_HALVES)
+        return f16 ? launch_kernel_of<BN, PAIR, 2, true, FUSE>(a, p, stream) : launch_kernel_of<BN, PAIR, 2, false, FUSE>(a, p, stream);
+    if (a.qk) return f16 ? launch_kernel_of<BN, PAIR, 1, true, FUSE>(a, p, stream) : launch_kernel_of<BN, PAIR, 1, false, FUSE>(a, p, stream);
+    return f16 ? launch_kernel_of<BN, PAIR, 0, true, FUSE>(a, p, stream) : launch_kernel_of<BN, PAIR, 0, false, FUSE>(a, p, stream);
 }
 
 std::atomic<int> g_mx_tile{0};  // 0: chosen per call; 64 / 128: single CTAs with that many columns; 512: CTA pairs
@@ -862,7 +941,7 @@ dirotq_status_t launch_mx_gemm(const MxGemmArgs& a, cudaStream_t stream) {
     p.ldy = a.ldy;
     p.status = a.status;
     p.early = a.early_weights;
-    p.wide_out = (reinterpret_cast<uintptr_t>(a.y) & 15u) == 0 && a.ldy % 8 == 0;
+    p.wide_out = (reinterpret_cast<uintptr_t>(a.y) & 15u) != 0 || a.ldy % 8 != 0 ? 0 : (reinterpret_cast<uintptr_t>(a.y) & 31u) != 0 || a.ldy % 16 != 0 ? 1 : 2;
     if (a.qk) {
         const dirotq_qk_t& qk = *a.qk;
         p.q_cols = qk.heads_q * qk.head_dim;
@@ -878,7 +957,7 @@ dirotq_status_t launch_mx_gemm(const MxGemmArgs& a, cudaStream_t stream) {
         p.cos_table = qk.cos_table;
         p.sin_table = qk.sin_table;
         p.ld_table = qk.ld_table;
-        p.wide_table = ((reinterpret_cast<uintptr_t>(qk.cos_table) | reinterpret_cast<uintptr_t>(qk.sin_table)) & 15u) == 0 && qk.ld_table % 4 == 0;
+        p.wide_table = ((reinterpret_cast<uintptr_t>(qk.cos_table) | reinterpret_cast<uintptr_t>(qk.sin_table)) & 31u) == 0 && qk.ld_table % 8 == 0;
         p.num_positions = qk.num_positions;
         p.positions = qk.positions;
     }
