@@ -24,7 +24,7 @@
 // the first).  With one kind of work left out at a time (12288 -> 12288, us per k-block of 256 rows x 256 columns): everything 0.40; no operand
 // loads 0.31, no MMAs 0.25, no scale copies 0.36, no outputs 0.37: loads into shared memory and the tensor core's reads of it share its
 // bandwidth, and neither a shorter hand-over (both CTAs' loads counted on the leader's barrier: 0.5 %) nor earlier releases of the accumulator
-// (0 %) change that.  4608 tokens of q/k/v (3 x 24 heads of 128): 74 us with norm and rotation, quantizer included, 59 without, 24 for the two as a pass.
+// (0 %) change that.  4608 tokens of q/k/v (3 x 24 heads of 128): 66 us with norm and rotation, quantizer included, 59 without, 24 for the two as a pass.
 #include "mxfp4.cuh"
 #include "ptx.cuh"
 
@@ -283,17 +283,49 @@ __device__ __forceinline__ void load_angles(const float* cs, const float* sn, in
     }
 }
 
+// What store_heads needs of its rows besides their values: positions, whether they are turned, and the angles of the rows that it turns next.
+template <int SETS, bool HALVES>
+struct HeadRows {
+    int pos[SETS][2];      // of row 16 set + 8 hi + l / 4
+    bool turned[SETS][2];
+    bool all;              // every row that exists is turned
+    float c[8], s[8];
+
+    __device__ __forceinline__ void start(const MxKernelParams& p, int row0, bool head, int at0, int lane) {
+        all = true;
+#pragma unroll
+        for (int set = 0; set < SETS; ++set)
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+                const int row = row0 + 16 * set + 8 * hi + (lane >> 2);
+                const bool here = head && row < p.M;
+                pos[set][hi] = here && p.positions != nullptr ? __ldg(p.positions + row) : row;
+                turned[set][hi] = here && (p.rope == DIROTQ_ROPE_NONE || (pos[set][hi] >= 0 && pos[set][hi] < p.num_positions));
+                all = all && (turned[set][hi] || !here);
+            }
+        if (head) fetch(p, 0, 0, at0, lane);
+    }
+    __device__ __forceinline__ void fetch(const MxKernelParams& p, int set, int hi, int at0, int lane) {
+        if (p.rope == DIROTQ_ROPE_NONE) return;
+        const long long a = static_cast<long long>(turned[set][hi] ? pos[set][hi] : 0) * p.ld_table + (HALVES ? at0 : at0 >> 1) + 8 * (lane & 3);
+        load_angles(p.cos_table + a, p.sin_table + a, p.wide_table, c, s);  // (row 0's where a row is not turned)
+    }
+};
+
 // The columns of a fused projection's tile that one warp has: two runs of 32 columns, at `run0` and `run1` of the group's, of SETS * 16 rows from
 // row0.  raw[set][run][4 k + 2 hi + e] is column 8 k + 2 t + e of the run, row 16 set + 8 hi + l / 4, and is so through bias, sum of squares and
-// norm; then the row's four lanes exchange it, so that each has whole sectors of the tables and of y (the bound here is the number of lines that
-// loads and stores touch: a row per lane, with half the instructions but 32 lines a load, took 79 us where this takes 7x).
+// norm, two fp32 operations at a time; then the row's four lanes exchange it, so that each has whole sectors of the tables and of y.  What counts here is
+// latency: with the angles loaded where they are used, 4608 tokens of 3 x 24 heads took 74 us, whether the tables were in L1 or not, with the next rows'
+// angles on their way 67, with the first rows' and the positions fetched behind the MMAs 66.  (A row per lane needs no exchange and half the instructions,
+// but touches 32 lines a load and store: 79 us, all loads at their use.)
 //   HALVES: element i and i + D/2 are in one warp: the runs are the halves of a head of 64 (run1 = run0 + 32), or halves of the halves of one of
 //           128 (run1 = run0 + 64); a lane has columns 8 t .. 8 t + 7 of both runs, which are turned with one another by eight angles.
 //   else:   64 columns side by side; a lane has columns 16 t .. 16 t + 15, eight pairs.
 // The two warps of a head of 128 (`split`) add up their sums of squares through s_sum, `pair_bar` their named barrier.
 template <int SETS, bool F16, bool HALVES>
-__device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], const MxKernelParams& p, int row0, int n0, int run0, int run1, bool split, int lane,
-                                            const float* s_b, const float* s_hw, float* s_sum, const float* s_sum_other, int pair_bar, uint32_t edge, bool whole) {
+__device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], HeadRows<SETS, HALVES>& rows_of, const MxKernelParams& p, int row0, int n0, int run0,
+                                            int run1, bool split, int lane, const float* s_b, const float* s_hw, float* s_sum, const float* s_sum_other, int pair_bar,
+                                            uint32_t edge, bool whole) {
     const int t = lane & 3, r4 = lane >> 2;
     const bool head = n0 + run0 < p.k_end;  // q or k (the same for the whole warp, and for the two of a head)
     const int at0 = run0 & ((1 << p.head_shift) - 1), at1 = run1 & ((1 << p.head_shift) - 1);  // the runs' places in the head
@@ -314,27 +346,6 @@ __device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], const 
                     split_pair(v, x, y);
                 }
         }
-    int pos[SETS][2];
-    bool turned[SETS][2], all = true;
-#pragma unroll
-    for (int set = 0; set < SETS; ++set)
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi) {
-            const int row = row0 + 16 * set + 8 * hi + r4;
-            const bool here = head && row < p.M;
-            pos[set][hi] = row;
-            if (here && p.positions != nullptr) pos[set][hi] = __ldg(p.positions + row);
-            turned[set][hi] = here && (p.rope == DIROTQ_ROPE_NONE || (pos[set][hi] >= 0 && pos[set][hi] < p.num_positions));
-            all = all && (turned[set][hi] || !here);
-        }
-    // A set's angles are on their way while the rows before it are packed and stored, the first's during the norm (row 0's where a row is not turned).
-    float c[8], s[8];
-    auto fetch = [&](int set, int hi) {
-        if (!head || p.rope == DIROTQ_ROPE_NONE) return;
-        const long long a = static_cast<long long>(turned[set][hi] ? pos[set][hi] : 0) * p.ld_table + (HALVES ? at0 : at0 >> 1) + 8 * t;
-        load_angles(p.cos_table + a, p.sin_table + a, p.wide_table, c, s);
-    };
-
     if (head && p.norm) {
         float ss[SETS][2];
 #pragma unroll
@@ -372,14 +383,13 @@ __device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], const 
                         for (int hi = 0; hi < 2; ++hi) {
                             uint32_t &x = raw[set][j][4 * k + 2 * hi], &y = raw[set][j][4 * k + 2 * hi + 1];
                             const uint64_t v = mul2(pair_of(x, y), mul2(pair_of(g.x, g.y), pair_of(ss[set][hi], ss[set][hi])));
-                            if (every || turned[set][hi]) split_pair(v, x, y);
+                            if (every || rows_of.turned[set][hi]) split_pair(v, x, y);
                         }
                 }
         };
-        if (__all_sync(0xffffffffu, all)) scale(true);
+        if (__all_sync(0xffffffffu, rows_of.all)) scale(true);
         else scale(false);
     }
-    fetch(0, 0);
 #pragma unroll
     for (int set = 0; set < SETS; ++set)
 #pragma unroll
@@ -404,7 +414,8 @@ __device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], const 
                     v[8 * j + 2 * k + 1] = odd[k];
                 }
             }
-            if (p.rope != DIROTQ_ROPE_NONE && turned[set][hi]) {
+            if (p.rope != DIROTQ_ROPE_NONE && rows_of.turned[set][hi]) {
+                const float(&c)[8] = rows_of.c, (&s)[8] = rows_of.s;
                 if constexpr (HALVES) {
 #pragma unroll
                     for (int k = 0; k < 8; k += 2) {
@@ -421,7 +432,7 @@ __device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], const 
                     }
                 }
             }
-            if (2 * set + hi + 1 < 2 * SETS) fetch(set + hi, hi ^ 1);
+            if (head && 2 * set + hi + 1 < 2 * SETS) rows_of.fetch(p, set + hi, hi ^ 1, at0, lane);  // on their way while these rows are packed and stored
             uint32_t o[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) o[k] = pack2<F16>(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
@@ -432,7 +443,8 @@ __device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], const 
                     store_run(p, row - r4, rows, n0 + (j ? run1 : run0), lane, make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]), edge, whole);
             } else if (whole && p.wide_out == 2) {
                 if (r4 < rows)
-                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row) * p.ldy + n0 + run0 + 16 * t),
+                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(
+                                     reinterpret_cast<uint16_t*>(p.y) + static_cast<long long>(row) * p.ldy + n0 + run0 + 16 * t),
                                  "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7])
                                  : "memory");
             } else {  // (lane t's 16 columns are run t / 2's, from 16 (t % 2): as halves of eight, in the order that store_run has them)
@@ -441,7 +453,8 @@ __device__ __forceinline__ void store_heads(uint32_t (&raw)[SETS][2][16], const 
                     uint32_t w4[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint32_t first = __shfl_sync(0xffffffffu, o[i], (lane & ~3) + 2 * j + (t >> 1)), other = __shfl_sync(0xffffffffu, o[4 + i], (lane & ~3) + 2 * j + (t >> 1));
+                        const int from = (lane & ~3) + 2 * j + (t >> 1);
+                        const uint32_t first = __shfl_sync(0xffffffffu, o[i], from), other = __shfl_sync(0xffffffffu, o[4 + i], from);
                         w4[i] = t & 1 ? other : first;
                     }
                     store_run(p, row - r4, rows, n0 + (j ? run1 : run0), lane, make_uint4(w4[0], w4[1], w4[2], w4[3]), edge, whole);
@@ -756,6 +769,12 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             // barrier orders the stores before the reads and makes the group agree on whether to go on
             float* s_b = reinterpret_cast<float*>(smem_gen + P::BIAS_OFFSET) + (group * 2 + (use & 1)) * 128;
             if (gt < CW) s_b[gt] = p.bias != nullptr && n0 + gt < p.N ? load_16(p.bias, n0 + gt, F16) : 0.f;
+            constexpr int SETS = HEADS128 ? 2 : 1;
+            const bool split = HEADS128 && p.head_shift == 7, apart = split && HEADS == 2;
+            const int run0 = HEADS128 ? (apart ? 32 : 64) * second : 0, run1 = run0 + (apart ? 64 : 32);
+            [[maybe_unused]] HeadRows<SETS, HEADS == 2> rows_of;
+            if constexpr (QKV)  // positions and the first angles come while the tile's MMAs run
+                rows_of.start(p, row0, n0 + run0 < p.k_end, run0 & ((1 << p.head_shift) - 1), lane);
             const bool failed = !mbar_wait(tfull_bar(acc), use & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
             if (group == 0 ? group_any<1, GROUP_THREADS>(failed) : group_any<2, GROUP_THREADS>(failed)) break;
             tc_fence_after_sync();
@@ -769,9 +788,6 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
                 else mbar_arrive(tempty_bar(acc));
             };
             if constexpr (QKV) {
-                constexpr int SETS = HEADS128 ? 2 : 1;
-                const bool split = HEADS128 && p.head_shift == 7, apart = split && HEADS == 2;
-                const int run0 = HEADS128 ? (apart ? 32 : 64) * second : 0, run1 = run0 + (apart ? 64 : 32);
                 uint32_t raw[SETS][2][16];
                 if (stored) {
 #pragma unroll
@@ -790,7 +806,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
                 if (!stored) continue;
                 float* sums = reinterpret_cast<float*>(smem_gen + P::SUM_OFFSET);
                 float *mine = sums + (warp - 4) * 32, *other = sums + ((warp - 4) ^ 4) * 32;
-                store_heads<SETS, F16, HEADS == 2>(raw, p, row0, n0, run0, run1, split, lane, s_b, s_hw, mine, other, 3 + group * 4 + q, edge, whole);
+                store_heads<SETS, F16, HEADS == 2>(raw, rows_of, p, row0, n0, run0, run1, split, lane, s_b, s_hw, mine, other, 3 + group * 4 + q, edge, whole);
             } else {
                 uint32_t raw[CH][32];  // [columns 64 c ..][4 j + 2 (row + 8) + (column + 1)], J = 8 c + j
                 if (stored) {
