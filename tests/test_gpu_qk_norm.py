@@ -225,6 +225,38 @@ def test_mxfp4_qkv_padding_tokens(M):
     assert torch.equal(y[pad], z[pad]) and torch.equal(y[:, 384:], z[:, 384:]) and not torch.equal(y[~pad], z[~pad])
 
 
+@pytest.mark.parametrize("M,hq,hk,D,style", [(9, 3, 2, 64, "halves"), (45, 3, 1, 128, "halves"), (150, 3, 1, 64, None), (270, 3, 2, 64, "halves"), (270, 2, 1, 128, "pairs"), (270, 2, 1, 128, "halves")])
+@pytest.mark.parametrize("columns", [0, 128, 512])
+def test_mxfp4_qkv_alignments_padding_and_plans(M, hq, hk, D, style, columns):
+    """One result whatever the alignment of y's rows (none, 16, 32 bytes), the tables' (none, 16, 32 bytes) and the plan; a token out of range keeps its projection."""
+    s = Setup(M, hq, hk, D, D if style else 0, style, torch.bfloat16, M + D)
+    if style:
+        s.positions[::5] = -1
+        s.positions[2::7] = len(s.cos)
+    g = torch.Generator().manual_seed(3)
+    x, w = torch.randn((M, 300), generator=g).bfloat16().cuda(), dq.dirotq_mxfp4_quantize((torch.randn((s.width, 300), generator=g) * 0.1).cuda())
+    ws = dq.alloc_mxfp4_workspace(M, 300)
+    y, z = (torch.empty((M, s.width), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dq.dirotq_mxfp4_qkv(x, w, y, ws, s.plan)
+    dq.dirotq_mxfp4_linear(x, w, z, ws)
+    pad = (s.positions < 0) | (s.positions >= len(s.cos)) if style else torch.zeros(M, dtype=torch.bool, device="cuda")
+    assert torch.equal(y[pad], z[pad]) and torch.equal(y[:, (hq + hk) * D:], z[:, (hq + hk) * D:]) and not torch.equal(y[~pad], z[~pad])
+    try:
+        dq.dirotq_set_gemm_tile(columns)
+        for more, extra in ((1, 1), (8, 4), (16, 8)):
+            wide = torch.full((2, len(s.cos), D // 2 + extra), 9.0, device="cuda")
+            wide[0, :, :D // 2], wide[1, :, :D // 2] = (s.cos, s.sin) if style else (0, 0)
+            kw = dict(rope=style, cos=wide[0, :, :D // 2], sin=wide[1, :, :D // 2], positions=s.positions) if style else {}
+            plan = dq.QkNorm(hq, hk, D, q_weight=s.wq, k_weight=s.wk, eps=s.eps, **kw)
+            out = torch.full((M + 1, s.width + more), 7, dtype=torch.bfloat16, device="cuda")
+            dq.dirotq_mxfp4_qkv(x, w, out[:M, :s.width], ws, plan)
+            assert torch.equal(out[:M, :s.width], y), more
+            assert bool((out[M] == 7).all()) and bool((out[:, s.width:] == 7).all())
+    finally:
+        dq.dirotq_set_gemm_tile(0)
+    assert dq.dirotq_workspace_status(ws) == 0
+
+
 @pytest.mark.parametrize("M,D", [(5, 64), (5, 128), (40, 64), (200, 64), (200, 128)])
 def test_mxfp4_qkv_bits_do_not_depend_on_the_plan(M, D):
     s = Setup(M, 4, 1, D, D, "halves", torch.bfloat16, 1)
