@@ -523,6 +523,7 @@ typedef struct {
     long long ld_table;
     int num_positions;
     const int32_t* positions;        /* DEVICE [M], or NULL: token m has position m (then num_positions >= M) */
+                                     /* (tables and positions are not looked at with DIROTQ_ROPE_NONE) */
 } dirotq_qk_t;
 
 /* x, q_out, k_out, v_out: one dtype (F32, BF16 or F16), 16-byte aligned, row strides ldx, ldq, ldk, ldv multiples of 8 elements.

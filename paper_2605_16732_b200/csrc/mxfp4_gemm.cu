@@ -27,6 +27,7 @@
 // (0 %) change that.  4608 tokens of q/k/v (3 x 24 heads of 128): 66 us with norm and rotation, quantizer included, 59 without, 24 for the two as a pass.
 #include "mxfp4.cuh"
 #include "ptx.cuh"
+#include "qk_plan.h"
 
 #include <atomic>
 #include <type_traits>
@@ -975,7 +976,7 @@ dirotq_status_t launch_mx_gemm(const MxGemmArgs& a, cudaStream_t stream) {
         p.ld_table = qk.ld_table;
         p.wide_table = ((reinterpret_cast<uintptr_t>(qk.cos_table) | reinterpret_cast<uintptr_t>(qk.sin_table)) & 31u) == 0 && qk.ld_table % 8 == 0;
         p.num_positions = qk.num_positions;
-        p.positions = qk.positions;
+        p.positions = qk_positions(qk);
     }
     const int plan = choose_plan(p.M, p.N, p.nkb, a.qk, sm_count(a.b->device));
     if (a.a == nullptr) return plan == 64 ? launch_plan<64, false, true>(a, p, stream) : launch_plan<128, false, true>(a, p, stream);

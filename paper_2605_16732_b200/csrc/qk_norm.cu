@@ -9,6 +9,7 @@
 // heads, and a sum over nine lanes is four steps of shuffle and test).  (One block of threads per token, weights and angles per head from memory: 67 us for the first.)
 #include "mxfp4.cuh"
 #include "ptx.cuh"
+#include "qk_plan.h"
 
 namespace dirotq {
 namespace {
@@ -395,7 +396,7 @@ cudaError_t launch_qk_norm_rope(const void* x, int dtype, int M, long long ldx, 
     p.cos_table = qk.cos_table; p.sin_table = qk.sin_table; p.ld_table = qk.ld_table;
     p.num_positions = qk.num_positions;
     p.wide_table = ((reinterpret_cast<uintptr_t>(qk.cos_table) | reinterpret_cast<uintptr_t>(qk.sin_table)) & 15u) == 0 && qk.ld_table % 4 == 0;
-    p.positions = qk.rope != DIROTQ_ROPE_NONE ? qk.positions : nullptr;
+    p.positions = qk_positions(qk);
     p.slots = slots; p.num_slots = num_slots;
     // v in its own place needs no copy
     const long long v_off = static_cast<long long>(qk.heads_q + qk.heads_kv) * qk.head_dim * static_cast<long long>(dtype_size(dtype));
