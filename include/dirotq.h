@@ -487,13 +487,15 @@ DIROTQ_API dirotq_status_t dirotq_mxfp4_export(const dirotq_mxfp4_t* t, uint8_t*
 /* y[m*ldy + n] = a[m,:] . b[n,:] + bias[n] for operands a [M,K] and b [N,K]: the block scales are applied inside the tensor core
  * (tcgen05.mma kind::mxf4), sums are held in fp32 and rounded once to y_dtype (BF16 or F16).  bias: DEVICE [N] in y's dtype, or NULL.
  * workspace: at least 256 bytes, 16-byte aligned, zero-filled once before its first use (dirotq_workspace_status reads it).
+ * y must not share memory with an operand, the bias or the workspace.
  * An output row's bits do not depend on how many rows the call has. */
 DIROTQ_API dirotq_status_t dirotq_mxfp4_gemm(const dirotq_mxfp4_t* a, const dirotq_mxfp4_t* b, const void* bias, void* y, int y_dtype,
                                              long long ldy, void* workspace, size_t workspace_bytes, dirotq_stream_t stream);
 
 /* A linear layer on a quantized weight w [N,K]: x (F32, BF16 or F16, x[m*ldx + k]) is quantized into the workspace, then
  * dirotq_mxfp4_gemm.  workspace: dirotq_mxfp4_workspace_bytes(M, K) bytes (enough for any smaller M too), 1024-byte aligned,
- * zero-filled once before its first use; calls that may overlap need distinct ones. */
+ * zero-filled once before its first use; calls that may overlap need distinct ones.  y may lie in x's memory, wholly or in part (all of x
+ * is read before any of y is written then), but not in that of w, the bias or the workspace. */
 DIROTQ_API dirotq_status_t dirotq_mxfp4_workspace_bytes(int M, int K, size_t* bytes);
 DIROTQ_API dirotq_status_t dirotq_mxfp4_linear(const void* x, int x_dtype, long long ldx, int M, int scale_rule, const dirotq_mxfp4_t* w,
                                                const void* bias, void* y, int y_dtype, long long ldy, void* workspace,
@@ -545,7 +547,7 @@ DIROTQ_API dirotq_status_t dirotq_linear_qkv(const void* x, int M, const dirotq_
 /* dirotq_mxfp4_linear on a fused q/k/v weight with norm and rotation in the product's epilogue: y = [q | k | v], rounded once.
  * head_dim 64 or 128, rot_dim 0 or head_dim; other heads: DIROTQ_ERR_UNSUPPORTED_SHAPE (dirotq_mxfp4_linear and dirotq_qk_norm_rope
  * serve those).  q and k of a token whose position is outside [0, num_positions) stay what the projection made them, as behind
- * dirotq_linear_qkv. */
+ * dirotq_linear_qkv.  y may lie in x's memory as for dirotq_mxfp4_linear, but not in that of qk's weights, tables or positions. */
 DIROTQ_API dirotq_status_t dirotq_mxfp4_qkv(const void* x, int x_dtype, long long ldx, int M, int scale_rule, const dirotq_mxfp4_t* w,
                                             const void* bias, const dirotq_qk_t* qk, void* y, int y_dtype, long long ldy,
                                             void* workspace, size_t workspace_bytes, dirotq_stream_t stream);

@@ -1,6 +1,7 @@
 // MXFP4 operands: handles, quantizer, dequantizer, plain import / export, and the entry points of the products.
 #include "mxfp4.cuh"
 #include "ptx.cuh"
+#include "row_ranges.h"
 
 #include <new>
 #include <type_traits>
@@ -419,7 +420,11 @@ dirotq_status_t linear(const void* x, int x_dtype, long long ldx, int M, int sca
     }
     st = check_operand(w);
     if (st != DIROTQ_OK) return st;
-    if (mx_fuses(M, w->rows, w->lay.nkb, qk, w->device)) {
+    // A product that quantizes x itself has blocks that write y while others still read x: with y in x's memory the quantizer runs alone, before
+    // anything of y is written, as it does for more rows.
+    const long long es = static_cast<long long>(dtype_size(x_dtype));
+    const bool apart = !rows_overlap(x, M, w->K * es, ldx * es, y, M, w->rows * 2ll, ldy * 2);
+    if (apart && mx_fuses(M, w->rows, w->lay.nkb, qk, w->device)) {
         const MxGemmArgs ga = {M, nullptr, x, x_dtype, ldx, scale_rule, w, bias, y, y_dtype, ldy, static_cast<int*>(workspace), false, qk};
         return launch_mx_gemm(ga, stream);
     }

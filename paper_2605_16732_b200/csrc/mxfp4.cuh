@@ -80,7 +80,7 @@ struct MxGemmArgs {
     const dirotq_qk_t* qk;   // norm and rotation in the epilogue, or NULL
 };
 dirotq_status_t launch_mx_gemm(const MxGemmArgs& a, cudaStream_t stream);
-bool mx_fuses(int M, int N, int nkb, const dirotq_qk_t* qk, int device);  // whether dirotq_mxfp4_linear / _qkv leaves x to the product's kernel
+bool mx_fuses(int M, int N, int nkb, const dirotq_qk_t* qk, int device);  // whether dirotq_mxfp4_linear / _qkv leaves x to the product's kernel (where y is not in x's memory)
 
 // qk_norm.cu
 dirotq_status_t qk_check(const dirotq_qk_t* qk, int M);

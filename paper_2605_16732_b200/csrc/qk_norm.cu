@@ -10,6 +10,7 @@
 #include "mxfp4.cuh"
 #include "ptx.cuh"
 #include "qk_plan.h"
+#include "row_ranges.h"
 
 namespace dirotq {
 namespace {
@@ -345,20 +346,6 @@ cudaError_t launch_t(QkParams& p, int M, cudaStream_t stream) {
 
 bool bad_float(float v) { return !(v >= 0.f) || v > 3.0e38f; }
 
-// Whether the rows [0, rows) of `width` bytes at `stride` bytes from a, and the rows of b, can share a byte: their whole ranges are compared,
-// and where both have the same stride, the columns as well.
-bool overlap(const void* a, long long rows_a, long long width_a, long long stride_a, const void* b, long long rows_b, long long width_b, long long stride_b) {
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-    const uintptr_t a1 = a0 + static_cast<uintptr_t>((rows_a - 1) * stride_a + width_a), b1 = b0 + static_cast<uintptr_t>((rows_b - 1) * stride_b + width_b);
-    if (a1 <= b0 || b1 <= a0) return false;
-    if (stride_a == stride_b) {
-        const uintptr_t s = static_cast<uintptr_t>(stride_a);
-        const uintptr_t off = (b0 >= a0 ? b0 - a0 : s - (a0 - b0) % s) % s;  // b's columns relative to a's
-        if (off >= static_cast<uintptr_t>(width_a) && off + static_cast<uintptr_t>(width_b) <= s) return false;
-    }
-    return true;
-}
-
 }  // namespace
 
 dirotq_status_t qk_check(const dirotq_qk_t* qk, int M) {
@@ -432,12 +419,12 @@ dirotq_status_t dirotq_qk_norm_rope(const void* x, int dtype, int M, long long l
     const bool q_in_place = static_cast<const void*>(q_out) == x && (ldq == ldx || M == 1);
     const bool k_in_place = static_cast<const char*>(k_out) == xb + wq * es && (ldk == ldx || M == 1) && !slots;
     const bool v_in_place = v_out && static_cast<const char*>(v_out) == xb + (wq + wk) * es && (ldv == ldx || M == 1) && !slots;
-    if (!q_in_place && overlap(x, M, xw, ldx * es, q_out, M, wq * es, ldq * es)) return DIROTQ_ERR_INVALID_ARG;
-    if (!k_in_place && overlap(x, M, xw, ldx * es, k_out, kv_rows, wk * es, ldk * es)) return DIROTQ_ERR_INVALID_ARG;
-    if (v_out && !v_in_place && overlap(x, M, xw, ldx * es, v_out, kv_rows, wk * es, ldv * es)) return DIROTQ_ERR_INVALID_ARG;
-    if (overlap(q_out, M, wq * es, ldq * es, k_out, kv_rows, wk * es, ldk * es)) return DIROTQ_ERR_INVALID_ARG;
-    if (v_out && (overlap(q_out, M, wq * es, ldq * es, v_out, kv_rows, wk * es, ldv * es) ||
-                  overlap(k_out, kv_rows, wk * es, ldk * es, v_out, kv_rows, wk * es, ldv * es)))
+    if (!q_in_place && rows_overlap(x, M, xw, ldx * es, q_out, M, wq * es, ldq * es)) return DIROTQ_ERR_INVALID_ARG;
+    if (!k_in_place && rows_overlap(x, M, xw, ldx * es, k_out, kv_rows, wk * es, ldk * es)) return DIROTQ_ERR_INVALID_ARG;
+    if (v_out && !v_in_place && rows_overlap(x, M, xw, ldx * es, v_out, kv_rows, wk * es, ldv * es)) return DIROTQ_ERR_INVALID_ARG;
+    if (rows_overlap(q_out, M, wq * es, ldq * es, k_out, kv_rows, wk * es, ldk * es)) return DIROTQ_ERR_INVALID_ARG;
+    if (v_out && (rows_overlap(q_out, M, wq * es, ldq * es, v_out, kv_rows, wk * es, ldv * es) ||
+                  rows_overlap(k_out, kv_rows, wk * es, ldk * es, v_out, kv_rows, wk * es, ldv * es)))
         return DIROTQ_ERR_INVALID_ARG;
     int dev = 0, major = 0;
     cudaError_t e = cudaGetDevice(&dev);
