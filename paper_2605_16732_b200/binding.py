@@ -893,8 +893,12 @@ def dirotq_qk_norm_rope(x: torch.Tensor, qk: QkNorm, q_out: torch.Tensor, k_out:
 
 
 def dirotq_linear_qkv(x: torch.Tensor, layer: Layer, y: torch.Tensor, workspace: torch.Tensor, qk: QkNorm, stream=None) -> None:
-    """dirotq_linear on a fused q/k/v layer, then norm and rotation of q and k in place on y."""
-    _check(lib().dirotq_linear_qkv(x.data_ptr(), x.shape[0], layer.handle, qk._ref(x.shape[0]), y.data_ptr(), workspace.data_ptr(), workspace.numel(),
+    """dirotq_linear on a fused q/k/v layer, then norm and rotation of q and k in place on y.  x: bf16 [M, K], y: bf16 [M, N], both contiguous."""
+    M, K = x.shape
+    assert K == layer.K and y.shape == (M, layer.N) and x.dtype is y.dtype is torch.bfloat16
+    assert x.is_contiguous() and y.is_contiguous(), "rows must be contiguous and side by side"
+    assert x.get_device() == y.get_device() == workspace.get_device() == layer.blob.get_device(), _OTHER_DEVICE
+    _check(lib().dirotq_linear_qkv(x.data_ptr(), M, layer.handle, qk._ref(M), y.data_ptr(), workspace.data_ptr(), workspace.numel(),
                                    _stream(stream)), "dirotq_linear_qkv")
 
 
