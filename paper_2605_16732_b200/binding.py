@@ -853,14 +853,18 @@ class QkNorm:
             assert positions is None or (positions.is_cuda and positions.is_contiguous() and positions.dtype == torch.int32 and positions.dim() == 1)
         self._tokens = None if positions is None else positions.numel()
         self._keep = (q_weight, k_weight, cos, sin, positions)
+        devices = {t.get_device() for t in self._keep if t is not None}
+        assert len(devices) <= 1, _OTHER_DEVICE
+        self._device = devices.pop() if devices else None
         self.struct = _QkStruct(heads_q, heads_kv, head_dim, int(norm), float(eps), _DTYPES[weights[0].dtype] if weights else DTYPE_F32, _ptr(q_weight),
                                 _ptr(k_weight), style, rot, _ptr(cos), _ptr(sin), _row_stride(cos, rot // 2) if style else 0, cos.shape[0] if style else 0,
                                 _ptr(positions))
         self._byref = ctypes.byref(self.struct)
         self._widths = heads_q * head_dim, heads_kv * head_dim
 
-    def _ref(self, M: int):
+    def _ref(self, M: int, device: int):
         assert self._tokens is None or self._tokens == M, "one position per token"
+        assert self._device is None or self._device == device, _OTHER_DEVICE
         return self._byref
 
 
@@ -886,7 +890,7 @@ def dirotq_qk_norm_rope(x: torch.Tensor, qk: QkNorm, q_out: torch.Tensor, k_out:
     else:
         assert slots.get_device() == device and slots.is_contiguous() and slots.dtype is torch.int32 and slots.numel() == M
         s_ptr, num_slots = slots.data_ptr(), rows
-    st = (_lib or lib()).dirotq_qk_norm_rope(x.data_ptr(), _DTYPES[dtype], M, ldx, qk._ref(M), q_out.data_ptr(), ldq, k_out.data_ptr(), ldk, v_ptr, ldv,
+    st = (_lib or lib()).dirotq_qk_norm_rope(x.data_ptr(), _DTYPES[dtype], M, ldx, qk._ref(M, device), q_out.data_ptr(), ldq, k_out.data_ptr(), ldk, v_ptr, ldv,
                                              s_ptr, num_slots, _stream(stream))
     if st:
         _check(st, "dirotq_qk_norm_rope")
@@ -898,7 +902,7 @@ def dirotq_linear_qkv(x: torch.Tensor, layer: Layer, y: torch.Tensor, workspace:
     assert K == layer.K and y.shape == (M, layer.N) and x.dtype is y.dtype is torch.bfloat16
     assert x.is_contiguous() and y.is_contiguous(), "rows must be contiguous and side by side"
     assert x.get_device() == y.get_device() == workspace.get_device() == layer.blob.get_device(), _OTHER_DEVICE
-    _check(lib().dirotq_linear_qkv(x.data_ptr(), M, layer.handle, qk._ref(M), y.data_ptr(), workspace.data_ptr(), workspace.numel(),
+    _check(lib().dirotq_linear_qkv(x.data_ptr(), M, layer.handle, qk._ref(M, x.get_device()), y.data_ptr(), workspace.data_ptr(), workspace.numel(),
                                    _stream(stream)), "dirotq_linear_qkv")
 
 
@@ -909,7 +913,7 @@ def dirotq_mxfp4_qkv(x: torch.Tensor, w: Mxfp4, y: torch.Tensor, workspace: torc
     N = w.rows
     assert K == w.K and y.shape == (M, N)
     assert x.get_device() == y.get_device() == workspace.get_device() == w.device, _OTHER_DEVICE
-    st = (_lib or lib()).dirotq_mxfp4_qkv(x.data_ptr(), _DTYPES[x.dtype], _row_stride(x, K), M, scale_rule, w.handle, _bias_ptr(bias, y, N), qk._ref(M),
+    st = (_lib or lib()).dirotq_mxfp4_qkv(x.data_ptr(), _DTYPES[x.dtype], _row_stride(x, K), M, scale_rule, w.handle, _bias_ptr(bias, y, N), qk._ref(M, w.device),
                                           y.data_ptr(), _DTYPES[y.dtype], _row_stride(y, N), workspace.data_ptr(), workspace.numel(), _stream(stream))
     if st:
         _check(st, "dirotq_mxfp4_qkv")

@@ -65,3 +65,59 @@ def test_tensors_on_another_device(recorder, name, width):
     with pytest.raises(AssertionError):
         _call(**{name: torch.zeros((M, width), **BF16).as_subclass(Elsewhere)})
     assert recorder.calls == []
+
+
+# ------------------------------------------------------------------ the description's own tensors
+
+class OnCuda(torch.Tensor):
+    """A tensor of the host's that says it is on GPU `where`."""
+    is_cuda = True
+
+    def get_device(self):
+        return self.where
+
+
+def _on(where, *shape, dtype=torch.float32):
+    t = torch.zeros(shape, dtype=dtype).as_subclass(OnCuda)
+    t.where = where
+    return t
+
+
+def _description(w_q=0, w_k=0, cos=0, sin=0, positions=0):
+    return dq.QkNorm(HQ, HK, D, q_weight=_on(w_q, D, **BF16), k_weight=_on(w_k, D, **BF16), rope="pairs", cos=_on(cos, 9, D // 2), sin=_on(sin, 9, D // 2),
+                     positions=_on(positions, M, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("name", ["w_q", "w_k", "cos", "sin", "positions"])
+def test_a_description_on_two_devices(name):
+    _description()
+    with pytest.raises(AssertionError):
+        _description(**{name: 1})
+
+
+def _norm_rope(where, qk):
+    rows = lambda n: _on(where, M, n * D, **BF16)
+    dq.dirotq_qk_norm_rope(rows(HQ + 2 * HK), qk, rows(HQ), rows(HK), rows(HK))
+
+
+def _mxfp4_qkv(where, qk):
+    w = dq.Mxfp4(None, _on(where, 4096, dtype=torch.uint8), N, K)
+    dq.dirotq_mxfp4_qkv(_on(where, M, K, **BF16), w, _on(where, M, N, **BF16), _on(where, 4096, dtype=torch.uint8), qk)
+
+
+def _linear_qkv(where, qk):
+    layer = dq.Layer(None, _on(where, 1024, dtype=torch.uint8), K, N, 16, 64)
+    dq.dirotq_linear_qkv(_on(where, M, K, **BF16), layer, _on(where, M, N, **BF16), _on(where, 4096, dtype=torch.uint8), qk)
+
+
+@pytest.mark.parametrize("call", [_norm_rope, _mxfp4_qkv, _linear_qkv])
+@pytest.mark.parametrize("where", [0, 1])
+def test_a_description_on_another_device_than_the_call(recorder, monkeypatch, call, where):
+    monkeypatch.setattr(dq, "_current_device", lambda: where)
+    call(where, dq.QkNorm(HQ, HK, D))  # (no tensors: right anywhere)
+    kw = dict.fromkeys(("w_q", "w_k", "cos", "sin", "positions"), where)
+    call(where, _description(**kw))
+    assert len(recorder.calls) == 2
+    with pytest.raises(AssertionError):
+        call(where, _description(**dict.fromkeys(kw, 1 - where)))
+    assert len(recorder.calls) == 2
