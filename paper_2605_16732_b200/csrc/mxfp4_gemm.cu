@@ -586,6 +586,9 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
 
     if (warp < 4) {
         if constexpr (SPLIT_REGS) reg_dealloc<32>();  // 128 * 32 + 512 * 112 registers are the 640 * 96 at launch
+        // (before these warps' first waits, all on what comes after the previous kernel: how long that one still runs is no part of a bounded wait.  The
+        // producer waits below, behind the loads that need not)
+        if (warp != 0) grid_dependency_wait();
         if (warp == 0) {
             // ------------------------------------------------------------ producer
             RingPos<STAGES> at;
