@@ -509,7 +509,8 @@ DIROTQ_API dirotq_status_t dirotq_mxfp4_linear(const void* x, int x_dtype, long 
  * and the first rot_dim elements of n are rotated in pairs (a, b) by the angle of the token's position p, c = cos_table[p][i],
  * s = sin_table[p][i], pair i:   (a, b) -> (a c - b s, a s + b c)
  *     DIROTQ_ROPE_PAIRS:  a = n[2i], b = n[2i+1];      DIROTQ_ROPE_HALVES:  a = n[i], b = n[i + rot_dim/2].
- * v is not changed.  Everything is computed in fp32 (the sum of squares too: |x| up to 1e18) and rounded once. */
+ * v is not changed.  Everything is computed in fp32 (the sum of squares too: |x| up to 1e18, and with eps == 0 the largest
+ * of a head at least 1e-17; a head of zeros is NaN then) and rounded once. */
 enum { DIROTQ_ROPE_NONE = 0, DIROTQ_ROPE_PAIRS = 1, DIROTQ_ROPE_HALVES = 2 };
 typedef struct {
     int heads_q, heads_kv, head_dim; /* head_dim a multiple of 8, at most 256 */
