@@ -124,8 +124,9 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_rows_kernel(const T* __r
 // ------------------------------------------------------------------ quantizer, elements along a column (weights stored [K, N])
 // A block of threads takes COLS * 32 columns x 256 elements along K: a thread has a block of 32 of one column (COLS = 1), or of two adjacent ones
 // in 16 bits (COLS = 2: pairs of values are loaded as words, so that a warp reads whole 128-byte lines either way).  Codes leave through
-// shared memory so that a column's 128 bytes are written together.  3072 x 12288 in fp32 31 us, 5.5 TB/s; 3072 x 9216 in bf16 15.5 us, 4.6 TB/s (43
-// with single 16-bit loads): memory.
+// shared memory so that a column's 128 bytes are written together.  With inputs that are not in L2: 3072 x 12288 in fp32 31.5 us, 5.4 TB/s, near the memory's
+// rate; 3072 x 9216 in bf16 19.8 us, 3.6 TB/s, and 23.1 with single 16-bit loads (9217 columns): not the memory there, but which of the 32 small loads a lane
+// has, the conversions and the exchange bounds it was not measured.
 template <typename T, int RULE, int COLS>
 __global__ void __launch_bounds__(kThreads) mx_quantize_cols_kernel(const T* __restrict__ x, long long ldx, int rows, int K, int nkb, int pitch,
                                                                     uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
@@ -276,7 +277,8 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* 
 }
 
 // ------------------------------------------------------------------ plain form of checkpoints
-// One thread per 32-bit word of the operand's codes (and its scale byte where it starts a block); bytes behind K become zeros.
+// One thread per 32-bit word of the operand's codes (and its scale byte where it starts a block); bytes behind K become zeros.  Once per checkpoint, by single
+// bytes, whose addresses may be odd: import of 9216 x 3072 23 us, 1.3 TB/s, export 60 us, 0.5 TB/s.
 __global__ void __launch_bounds__(kThreads) mx_import_kernel(const uint8_t* __restrict__ in_codes, const uint8_t* __restrict__ in_scales, int rows, int K,
                                                              int nkb, int pitch, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
     const int words = nkb * 32;

@@ -10,7 +10,7 @@
 // to the MMA warp through an mbarrier.  An atom's 32-bit words hold the scales of two instructions; the instruction descriptor's scale
 // ids (0 or 2) pick the half.
 //
-// Roles: warp 0 TMA producer, warp 1 MMA issuer and owner of the tensor memory, warps 2..3 scale copiers, 16 (or 8) epilogue warps in two
+// Roles: warp 0 TMA producer, warp 1 MMA issuer and owner of the tensor memory, warps 2..3 scale copiers, 16 epilogue warps in two
 // groups.  Plans:
 //   PAIR: clusters of two CTAs share every MMA (cta_group::2, M = 256): 256 rows x 256 columns per pair; each CTA holds its own 128 rows of
 //         a, half of b's 256 rows, and the scales of both halves.  One 256-column accumulator, an epilogue group per half of it: the group
@@ -20,8 +20,8 @@
 //         their codes and scales stay; the ring carries b alone.
 // Every plan adds an output element's products in the same order, so that a row's bits do not depend on the plan.
 //
-// Measured: 4608 rows, 3072 -> 12288 68 us, 5.1 PFLOP/s; 12288 -> 3072 56 us, 6.2 PFLOP/s (pairs, 1.97 GHz; at the power cap of a long run, 1.6 GHz, 83 us for
-// the first).  With one kind of work left out at a time (12288 -> 12288, us per k-block of 256 rows x 256 columns): everything 0.40; no operand
+// Measured: 4608 rows, 3072 -> 12288 68 us, 5.1 PFLOP/s; 12288 -> 3072 56 us, 6.2 PFLOP/s (pairs, 1.97 GHz; at the power cap, after
+// seconds of it, 1.45 GHz, 84 and 72 us).  With one kind of work left out at a time (12288 -> 12288, us per k-block of 256 rows x 256 columns): everything 0.40; no operand
 // loads 0.31, no MMAs 0.25, no scale copies 0.36, no outputs 0.37: loads into shared memory and the tensor core's reads of it share its
 // bandwidth, and neither a shorter hand-over (both CTAs' loads counted on the leader's barrier: 0.5 %) nor earlier releases of the accumulator
 // (0 %) change that.  4608 tokens of q/k/v (3 x 24 heads of 128): 66 us with norm and rotation, quantizer included, 59 without, 24 for the two as a pass.
@@ -46,8 +46,9 @@ template <int BN, bool PAIR, bool FUSE>
 struct MxPlan {
     static constexpr int NB = BN == 256 ? 2 : 1;                              // 128-column blocks whose scales a stage holds
     // k-blocks per stage: two where a k-block is little work, so that a short call pays for the roles' waits and hand-overs half as often
-    // (128 rows, 12288 -> 3072: 9.6 against 10.3 us; 16 rows, 3072 -> 9216: 6.4 against 6.9 with the quantizer).  What is left at 64 columns,
-    // 0.15 us a k-block, is its four MMAs, each of which waits for the one before: they add to the same accumulator in order.
+    // (128 rows, 12288 -> 3072: 9.6 against 10.3 us; 16 rows, 3072 -> 9216: 6.4 against 6.9 with the quantizer).  What is left at 64 columns
+    // is 0.15 us a k-block; whether its four MMAs, which add to one accumulator in order, take that or their operands' way into shared memory was not
+    // measured apart.
     static constexpr int KBS = BN == 64 || FUSE ? 2 : 1;
     static constexpr int A_STAGE = FUSE ? 0 : A_BYTES;
     static constexpr int B_BYTES = (PAIR ? BN / 2 : BN) * 128;                // this CTA's rows of b: the tile's (single) or half of them (pair)
@@ -913,6 +914,8 @@ bool fuse_fits(int M, int nkb) {
 // Columns per tile of single CTAs, or 512 for pairs: the shortest schedule, turns of the SMs x the time of a tile.  Microseconds a tile of nkb
 // k-blocks takes, from calls of one to nine turns: 64 columns 0.30 + 0.17 nkb, 128 columns 0.55 + 0.235 nkb, pairs 1.0 + 0.36 nkb and 1.3
 // once (clusters start later).  (512 rows, K 1152 -> 1152: 3.5, 4.4, 6.2 us; 512 rows, 3072 -> 9216: 11.9, 9.2, 9.6; 4608 rows: pairs 50.)
+// Norm and rotation in the epilogue are in none of the three: for 3 x 24 heads of 128 and K = 3072 they move the border between 128 columns and pairs up:
+// linear, quantizer included, 512 tokens 12.7 / 12.7 us (128 columns / pairs), 1024 19.3 / 17.4; q/k/v 14.0 / 14.6, 19.9 / 20.2, and 2048 34.6 / 30.8.
 int choose_plan(int M, int N, int nkb, const dirotq_qk_t* qk, int sms) {
     const bool heads_of_128 = qk != nullptr && qk->head_dim == 128;  // (a tile's columns are whole heads)
     const int forced = g_mx_tile.load();

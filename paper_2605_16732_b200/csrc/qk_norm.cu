@@ -6,7 +6,9 @@
 //
 // Measured (bf16, q, k and v copied): 4608 tokens, 3 x 24 heads of 128, 30.7 us, 5.5 TB/s; 18432 tokens 6.1 TB/s; heads of 64 15.0 us; 64 tokens of 32 + 2 x 8
 // heads 3.0 us (latency).  4173 tokens, 3 x 16 heads of 72 in fp16, half of each turned: 15 us, 3.9 TB/s: instructions (27 of 32 lanes hold
-// heads, and a sum over nine lanes is four steps of shuffle and test).  (One block of threads per token, weights and angles per head from memory: 67 us for the first.)
+// heads, and a sum over nine lanes is four steps of shuffle and test).  Heads of other sizes, 4608 tokens, tensors that are not in L2, all of a head turned:
+// 3 x 16 heads of 80 23 us, 3.1 TB/s; 3 x 24 of 96 36, 3.5; 3 x 16 of 160 47, 3.0; 3 x 8 of 256 28, 4.0; 3 x 32 of 32 15, 3.8.
+// (One block of threads per token, weights and angles per head from memory: 67 us for the first.)
 #include "mxfp4.cuh"
 #include "ptx.cuh"
 #include "qk_plan.h"
@@ -120,7 +122,10 @@ __device__ __forceinline__ float weight_at(const void* p, int i, int dtype) {
 template <typename T>
 constexpr int kHeads = sizeof(T) == 4 ? 2 : 4;  // sets of heads a warp takes at once
 
-// STYLE; LANES: lanes of a head where head_dim is 64, 72 or 128, 0: p.L, any.
+// STYLE; LANES: lanes of a head where head_dim is 64, 72 or 128, 0: p.L, any.  The three are sizes of the models whose layers the library serves; a constant
+// unrolls the sum over a head's lanes and, in the QUARTER and HALVES styles, keeps registers from spilling.  4608 tokens, tensors that are not in L2, constant
+// against p.L, us: heads of 64 all turned in pairs 31.5 / 35.2, a half turned in halves 32.3 / 42.1, a third 35.2 / 46.5; of 72 20.2 / 22.5, 20.1 / 24.7, 23.7 / 30.6;
+// of 128 31.9 / 36.5, 32.9 / 44.2, 36.2 / 49.4; 64 tokens 0.3 to 1.2 us apart.
 template <typename T, int STYLE, int LANES>
 __global__ void __launch_bounds__(kThreads, STYLE == HALVES && sizeof(T) == 4 ? 2 : 3) qk_norm_rope_kernel(const __grid_constant__ QkParams p) {
     constexpr int HEADS = kHeads<T>;
@@ -319,7 +324,11 @@ cudaError_t launch_t(QkParams& p, int M, cudaStream_t stream) {
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     // A warp's turn takes all sets of a token's q, k or v where that leaves every SM 32 turns, so that angles and weights are fetched once for
-    // all of them; with fewer tokens one set, so that the call is over sooner.
+    // all of them; with fewer tokens one set, so that the call is over sooner.  One set against all, us, for 64, 512, 1024, 2048, 2368 (from here
+    // on: all), 4608, 9216 tokens: 3 x 24 heads of 128 3.4 / 5.9, 7.0 / 7.5, 10.8 / 9.5, 18.3 / 17.0, 20.4 / 18.5, 34.9 / 32.0, 63.2 / 58.6; 3 x 16 of 72
+    // 3.1 / 3.8, 4.6 / 5.6, 7.7 / 6.7, 12.4 / 11.4, 13.1 / 11.7, 21.6 / 20.0, 39.2 / 35.4.  With four q heads to one of k and v turns are of unequal
+    // length, and all loses up to between 4608 and 9216 tokens: 32 + 2 x 8 heads of 128 3.2 / 6.7, 5.0 / 8.2, 8.2 / 9.6, 13.0 / 16.6, 14.3 / 17.4,
+    // 25.9 / 29.0, 46.7 / 44.0.
     const int per = kHeads<T> * p.per_warp, sets_q = (p.hq + per - 1) / per, sets_k = (p.hk + per - 1) / per;
     const bool whole = static_cast<long long>(M) * 2 >= 32ll * sm_count(device);
     p.part_sets = whole ? (sets_q > sets_k ? sets_q : sets_k) : 1;
