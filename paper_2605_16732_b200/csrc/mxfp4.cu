@@ -13,6 +13,10 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// The quantizers' x and the dequantizer's codes and scales may be what the previous kernel of the stream still writes when these start (dependent launches).  They
+// carry no __restrict__: it makes them loads of constant memory, which nothing holds behind the wait for that kernel.  (Where such loads are faster, columns of
+// 32-bit weights 24 against 25 us, their addresses are.)
+
 // ------------------------------------------------------------------ quantizer, elements along a row
 // A unit is 512 elements of a row (four scale words).  A warp takes UNITS of them, sixteen elements per lane and unit, their loads in flight
 // together: two lanes share a block of 32, so its maximum is one shuffle and a scale word three; codes leave as 8 bytes a lane, 256 a warp.  In
@@ -70,8 +74,8 @@ __device__ __forceinline__ Raw16<T> load_raw16(const T* row, int k0, int K) {
 }
 
 template <typename T, int RULE, int ALIGN, int UNITS>
-__global__ void __launch_bounds__(kThreads) mx_quantize_rows_kernel(const T* __restrict__ x, long long ldx, int rows, int K, int nkb, int pitch,
-                                                                    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+__global__ void __launch_bounds__(kThreads) mx_quantize_rows_kernel(const T* x, long long ldx, int rows, int K, int nkb, int pitch,
+                                                                    uint8_t* codes, uint8_t* scales) {
     const int lane = threadIdx.x & 31;
     const int per_row = (nkb + 1) >> 1;
     const unsigned units = static_cast<unsigned>(rows) * per_row;  // (at most 2^31 - 1, see check_shape)
@@ -128,8 +132,8 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_rows_kernel(const T* __r
 // rate; 3072 x 9216 in bf16 19.8 us, 3.6 TB/s, and 23.1 with single 16-bit loads (9217 columns): not the memory there, but which of the 32 small loads a lane
 // has, the conversions and the exchange bounds it was not measured.
 template <typename T, int RULE, int COLS>
-__global__ void __launch_bounds__(kThreads) mx_quantize_cols_kernel(const T* __restrict__ x, long long ldx, int rows, int K, int nkb, int pitch,
-                                                                    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+__global__ void __launch_bounds__(kThreads) mx_quantize_cols_kernel(const T* x, long long ldx, int rows, int K, int nkb, int pitch,
+                                                                    uint8_t* codes, uint8_t* scales) {
     constexpr int WIDTH = 32 * COLS;
     __shared__ uint4 s_codes[WIDTH][9];  // (a piece of padding: the threads of a warp write different columns' rows)
     __shared__ __align__(16) uint8_t s_scales[WIDTH][8];
@@ -138,13 +142,14 @@ __global__ void __launch_bounds__(kThreads) mx_quantize_cols_kernel(const T* __r
     const int row0 = blockIdx.x / nkb * WIDTH;
     const int row = row0 + lane * COLS, k0 = kb * 256 + w * 32;
     grid_dependency_wait();
+    asm volatile("" : "+l"(x));  // (no address of x is known before this point: none of the loads below can be moved ahead of the wait)
     grid_launch_dependents();
     using Word = std::conditional_t<COLS == 2, uint32_t, T>;
     Word raw[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
         raw[i] = Word();
-        if (row < rows && k0 + i < K) raw[i] = *reinterpret_cast<const Word*>(x + (k0 + i) * ldx + row);
+        if (row < rows && k0 + i < K) raw[i] = __ldg(reinterpret_cast<const Word*>(x + (k0 + i) * ldx + row));
     }
 #pragma unroll
     for (int c = 0; c < COLS; ++c) {
@@ -226,8 +231,8 @@ __device__ __forceinline__ void store_unit(T* row, int k0, int K, const Raw16<T>
 }
 
 template <typename T, int ALIGN, int UNITS>
-__global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int K,
-                                                                 int nkb, int pitch, T* __restrict__ y, long long ldy) {
+__global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t* codes, const uint8_t* scales, int rows, int K,
+                                                                 int nkb, int pitch, T* y, long long ldy) {
     const int lane = threadIdx.x & 31;
     const int per_row = (nkb + 1) >> 1;
     const unsigned units = static_cast<unsigned>(rows) * per_row;
