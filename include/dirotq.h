@@ -16,6 +16,8 @@
  *   - Every tensor pointer is a DEVICE pointer owned by the caller unless the name says `host`.
  *     The library allocates no device memory.  `stream` is a cudaStream_t passed as void*.
  *   - Calls enqueue work on `stream` and return without synchronising, unless stated.
+ *   - Calls may come from several host threads at once (with workspaces of their own), and be the first thing that their thread
+ *     does on the device.
  *   - Argument errors are reported before anything is launched.  A CUDA launch error is
  *     returned as DIROTQ_ERR_CUDA.  Device-side waits are bounded; when one expires the kernel
  *     records a code in the workspace status word (see dirotq_workspace_status) and returns.
